@@ -403,6 +403,123 @@ int32_t mtla_pages_fork(mtla_page_book* book, const int32_t* src_index /*host*/,
                         int32_t* fresh_pages /*host*/);
 
 /*
+ * Page tables on the device -- the bookkeeping of mtla_pages_reserve for callers that cannot bring the lengths to
+ * the host: a serving loop replayed as a HIP graph, whose requests take and give back pages while it runs.  One
+ * pool of pages, all arrays DEVICE memory of the caller's (of the structure itself the call keeps nothing):
+ *   table   int32 [max_batch, max_pages]   what the _paged calls take as page_table
+ *   first, end  int32 [max_batch]          entries first .. end - 1 of a sequence's row name the pages it holds
+ *   ring    int32 [n_pages]                free pages, `count` of them from place `head` on (wrapping round)
+ *   state   int32 [4]                      head, count, sequences refused by the last call, 0
+ *   was_end int32 [max_batch] or NULL      written: `end` as it was before the last call
+ *   spill   a page outside the ring, or -1: see below
+ * A pool nobody holds a page of: first and end 0, ring the page numbers in any order, state {0, n_pages, 0, 0}.  A
+ * page belongs to one sequence (no beams share it: they keep their pages with mtla_pages_fork).
+ */
+typedef struct {
+  int32_t* table;
+  int32_t* first;
+  int32_t* end;
+  int32_t* ring;
+  int32_t* state;
+  int32_t* was_end; /* nullable */
+  int32_t n_pages;
+  int32_t spill;
+} mtla_page_pool;
+
+/*
+ * mtla_pages_fit -- makes the tables of sequences 0 .. batch-1 fit their lengths: a sequence of seq_len[b] tokens that
+ * n_new[b] (NULL: n_new_max; values are clamped to [0, n_new_max]) are about to join holds afterwards, with P =
+ * page_slots and lengths outside [0, max_slots s] counted as the nearer end,
+ *   packed != NULL, in `packed`   entries [0, c),  c = max(seq_len / s / P - keep_pages, 0): its complete pages but
+ *                                 the newest keep_pages
+ *   in `pool`                     entries [c, ceil(ceil((seq_len + n_new) / s) / P)), the rest; c = 0 without `packed`
+ * Pages it lacks come out of the ring in the order of sequences and entries; pages it has no use for (also all
+ * those of a sequence whose length was set to 0) go back behind the ring's last page in that order, and their
+ * table entries keep naming them, so that mtla_pages_pack can still read what this call moved to `packed`.  They
+ * are handed out again from the NEXT call on.
+ * Order of a step over packed pages: mtla_pages_fit(n_new_max = 1), mtla_pages_pack(first = packed->was_end, end =
+ * packed->end), mtla_decode_step_packed with n_packed = packed->end.
+ * Refusal: a sequence gets all the pages it lacks in a pool, or none where the ring does not hold what it and the
+ * sequences before it lack together.  It then keeps what it holds of what it should hold, MTLA_ERR_CAPACITY is
+ * raised in the workspace header, and state[2] counts such sequences.  In `packed` nothing is lost by that: `pool`
+ * keeps the pages (c becomes the packed end it has) until a later call finds room.  In `pool` the sequence has no
+ * page for its new tokens; with spill >= 0 its missing entries name that page, so that an append that nobody
+ * held back writes there and not into another sequence's page.
+ * A length may fall, to 0 or by tokens that are dropped, as long as the page it falls into is not a packed one
+ * (mtla_pages_unpack first, or keep_pages >= 1).
+ *
+ *   slot_map   device int64 [batch, n_new_max] or NULL: the row of the pool (page * page_slots + slot in it) that
+ *              token t of sequence b goes to; -1 for padding, beyond the capacity, and for a refused sequence's
+ *              tokens without a page
+ *   workspace  device, the context's workspace (status word)
+ */
+mtla_status mtla_pages_fit(mtla_ctx* ctx, const mtla_page_pool* pool, const mtla_page_pool* packed /*nullable*/,
+                           const int32_t* seq_len, const int32_t* n_new, int32_t n_new_max, int32_t keep_pages,
+                           int32_t batch, int64_t* slot_map, void* workspace, void* hip_stream);
+
+/*
+ * Packed pages -- complete pages of paged storage in 4 bits (a complete slot never changes, so a complete page is
+ * rounded once).  A row's latents are 4-bit floats (E2M1: 0, .5, 1, 1.5, 2, 3, 4, 6 and their negatives) times one power
+ * of two per 32 of them (E8M0: exponent + 127), its RoPE key stays bf16: r/2 + r/32 + 2 d_rope bytes a slot
+ * instead of 2 (r + d_rope).  The power of two is the smallest of which the block's largest magnitude is at most
+ * the seven-fold, between 2^-124 and 2^125; numbers go to the nearest, ties to the even code, beyond 6 to 6.  An
+ * infinity or NaN makes its block NaN (scale 255).  Layout, in tiles of 16 slots:
+ *   codes   uint8 [n_pages, page_slots / 16, r / 32, 16, 16]     32 latents of a slot, the even ones in the low nibbles
+ *   scales  uint8 [n_pages, page_slots / 16, r / 32, 16]
+ *   keys    elem  [n_pages, page_slots / 16, d_rope / 8, 16, 8]
+ *   table      device int32 [max_batch, max_pages]: entry k < n_packed[b] names the packed page of logical page k
+ *   n_packed   device int32 [batch]: pages of a sequence that the decode calls read here, taken as
+ *              [0, max_pages]; its further pages are those of page_table.  (mtla_pages_pack / _unpack: may be NULL)
+ *   n_pages    of the three arrays; n_pages * page_slots < 2^31.  Table entries are clamped into [0, n_pages).
+ */
+typedef struct {
+  void* codes;
+  void* scales;
+  void* keys;
+  const int32_t* table;
+  const int32_t* n_packed;
+  int32_t n_pages;
+} mtla_packed_cache;
+
+size_t mtla_packed_codes_bytes(const mtla_ctx* ctx, int32_t n_pages);
+size_t mtla_packed_scales_bytes(const mtla_ctx* ctx, int32_t n_pages);
+size_t mtla_packed_keys_bytes(const mtla_ctx* ctx, int32_t n_pages);
+
+/*
+ * mtla_pages_pack, mtla_pages_unpack -- logical pages first[b] .. end[b] - 1 of sequences 0 .. batch-1 from the bf16
+ * pool (page_table) into packed pages (pk->table), or back; the way back is exact.  first NULL: 0; both are taken
+ * inside [0, max_pages].  Nothing else is read or written; both forms of a page may go on to be used.
+ *   pages_each  host: pages that a sequence is expected to have in this call.  Sizes the launch; any number is moved.
+ * Two sequences may name one source page; a destination page named twice holds either.
+ */
+mtla_status mtla_pages_pack(mtla_ctx* ctx, const void* cache_c, const void* cache_kr, const int32_t* page_table,
+                            const mtla_packed_cache* pk, const int32_t* first, const int32_t* end, int32_t batch,
+                            int32_t pages_each, void* hip_stream);
+mtla_status mtla_pages_unpack(mtla_ctx* ctx, void* cache_c, void* cache_kr, const int32_t* page_table,
+                              const mtla_packed_cache* pk, const int32_t* first, const int32_t* end, int32_t batch,
+                              int32_t pages_each, void* hip_stream);
+
+/*
+ * mtla_decode_attn_packed, mtla_decode_step_packed -- mtla_decode_attn_paged and mtla_decode_step_paged over both
+ * kinds of page: slots below n_packed[b] * page_slots out of the packed pages, the others out of page_table's.  The
+ * step appends through page_table, so the page that its token goes to must not be a packed one (mtla_pages_fit
+ * sees to that).  Arguments, checks and errors as there, any n_heads and d_head, but
+ *   out   device elem [batch, n_heads, d_head] or NULL: bf16, what W_O's product takes; its rounding is the largest
+ *         error behind the packing (sums, weights and normalisers are fp32 or better than 16 bits)
+ * mtla_set_decode_chunk applies; mtla_set_decode_schedule does not.  Not together with mtla_set_shared_prefix
+ * (MTLA_ERR_UNSUPPORTED).
+ */
+mtla_status mtla_decode_attn_packed(mtla_ctx* ctx, const void* q, const void* q_rope, const void* w_uk, const void* w_uv,
+                                    const void* cache_c, const void* cache_kr, const int32_t* seq_len,
+                                    const int32_t* page_table /*device*/, const mtla_packed_cache* pk, int32_t batch,
+                                    void* out, float* out_latent, float* lse, void* workspace, void* hip_stream);
+mtla_status mtla_decode_step_packed(mtla_ctx* ctx, void* cache_c, void* cache_kr, float* tail_c, int32_t* seq_len,
+                                    const int32_t* page_table /*device*/, const mtla_packed_cache* pk, const void* c_new,
+                                    const void* kr_new, const void* hyp_A, const void* hyp_a, const void* hyp_G,
+                                    const void* q, const void* q_rope, const void* w_uk, const void* w_uv, int32_t batch,
+                                    void* out, float* out_latent, float* lse, void* workspace, void* hip_stream);
+
+/*
  * mtla_set_shared_prefix -- decoding several beams over one stored copy of what
  * they have in common (the appendix on decoding with beams of 10-50: every
  * hypothesis of an utterance starts from the same tokens).  While set, the

@@ -40,6 +40,43 @@ class mtla_page_book(C.Structure):
     _fields_ += [(n, C.c_int32) for n in ("max_batch", "max_pages", "n_pages", "page_slots", "stride", "max_slots")]
 
 
+def _device_array(name, t, dtype, dims=None):
+    """The address of a tensor that the library's kernels follow: on a device, dense, of the type that they read."""
+    import torch
+    want = getattr(torch, dtype)
+    if not isinstance(t, torch.Tensor) or t.dtype != want or not t.is_contiguous() or (dims is not None and t.dim() != dims):
+        raise TypeError(f"{name}: a dense {dtype} tensor{'' if dims is None else f' of {dims} dimensions'} is needed")
+    return t.data_ptr()
+
+
+class PagePool(C.Structure):
+    """mtla_page_pool over the caller's tensors, which it keeps alive."""
+    _fields_ = [(n, C.c_void_p) for n in ("table", "first", "end", "ring", "state", "was_end")] + [("n_pages", C.c_int32), ("spill", C.c_int32)]
+
+    def __init__(self, table, first, end, ring, state, was_end=None, spill: int = -1):
+        at = [_device_array(n, t, "int32", d) for n, t, d in (("table", table, 2), ("first", first, 1), ("end", end, 1), ("ring", ring, 1),
+                                                               ("state", state, 1))]
+        at.append(None if was_end is None else _device_array("was_end", was_end, "int32", 1))
+        if any(t is not None and t.numel() != table.shape[0] for t in (first, end, was_end)) or state.numel() < 4:
+            raise ValueError("first, end and was_end have an entry per row of the table, state has four")
+        super().__init__(*at, ring.numel(), spill)
+        self.tensors = dict(table=table, first=first, end=end, ring=ring, state=state, was_end=was_end)
+
+
+class PackedCache(C.Structure):
+    """mtla_packed_cache over the caller's tensors, which it keeps alive (n_packed may be None for pack and unpack)."""
+    _fields_ = [(n, C.c_void_p) for n in ("codes", "scales", "keys", "table", "n_packed")] + [("n_pages", C.c_int32)]
+
+    def __init__(self, codes, scales, keys, table, n_packed=None):
+        at = [_device_array(n, t, d) for n, t, d in (("codes", codes, "uint8"), ("scales", scales, "uint8"), ("keys", keys, "bfloat16"),
+                                                      ("table", table, "int32"))]
+        n_pages = codes.shape[0]
+        if scales.shape[0] != n_pages or keys.shape[0] != n_pages or codes.numel() != 16 * scales.numel():
+            raise ValueError("codes, scales and keys are of the same pages")
+        super().__init__(*at, None if n_packed is None else _device_array("n_packed", n_packed, "int32", 1), n_pages)
+        self.tensors = dict(codes=codes, scales=scales, keys=keys, table=table, n_packed=n_packed)
+
+
 class MtlaError(RuntimeError):
     def __init__(self, status: int, where: str):
         self.status = status
@@ -84,6 +121,14 @@ SIGNATURES = {
     "mtla_pages_reserve": (_i32, [C.POINTER(mtla_page_book), _vp, _i32]),
     "mtla_pages_fork": (_i32, [C.POINTER(mtla_page_book), _vp, _i32, _vp]),
     "mtla_cache_fork_paged": (C.c_int, [_ctx] + [_vp] * 7 + [_i32] + [_vp] * 5),
+    "mtla_pages_fit": (C.c_int, [_ctx, C.POINTER(PagePool), C.POINTER(PagePool), _vp, _vp, _i32, _i32, _i32, _vp, _vp, _vp]),
+    "mtla_packed_codes_bytes": (_sz, [_ctx, _i32]),
+    "mtla_packed_scales_bytes": (_sz, [_ctx, _i32]),
+    "mtla_packed_keys_bytes": (_sz, [_ctx, _i32]),
+    "mtla_pages_pack": (C.c_int, [_ctx, _vp, _vp, _vp, C.POINTER(PackedCache), _vp, _vp, _i32, _i32, _vp]),
+    "mtla_pages_unpack": (C.c_int, [_ctx, _vp, _vp, _vp, C.POINTER(PackedCache), _vp, _vp, _i32, _i32, _vp]),
+    "mtla_decode_attn_packed": (C.c_int, [_ctx] + [_vp] * 8 + [C.POINTER(PackedCache), _i32] + [_vp] * 5),
+    "mtla_decode_step_packed": (C.c_int, [_ctx] + [_vp] * 5 + [C.POINTER(PackedCache)] + [_vp] * 9 + [_i32] + [_vp] * 5),
     "mtla_workspace_bytes": (_sz, [_ctx]),
     "mtla_prefill_workspace_bytes": (_sz, [_ctx, _i32, _i32]),
     "mtla_workspace_init": (C.c_int, [_ctx, _vp, _vp]),
@@ -276,6 +321,36 @@ class Context:
                                 dst_table, dst_tail_c, dst_seq_len, workspace, stream=None) -> int:
         return calls.mtla_cache_fork_paged(self._ptr, cache_c, cache_kr, src_table, src_tail_c, src_seq_len, src_index,
                                            fresh_pages, batch, dst_table, dst_tail_c, dst_seq_len, workspace, stream)
+
+    # page tables on the device, packed pages
+    def pages_fit_status(self, pool, packed, seq_len, n_new, n_new_max, keep_pages, batch, slot_map, workspace, stream=None) -> int:
+        return calls.mtla_pages_fit(self._ptr, pool, packed, seq_len, n_new, n_new_max, keep_pages, batch, slot_map, workspace, stream)
+
+    def pages_pack_status(self, cache_c, cache_kr, page_table, packed_cache, first, end, batch, pages_each, stream=None) -> int:
+        return calls.mtla_pages_pack(self._ptr, cache_c, cache_kr, page_table, packed_cache, first, end, batch, pages_each, stream)
+
+    def pages_unpack_status(self, cache_c, cache_kr, page_table, packed_cache, first, end, batch, pages_each, stream=None) -> int:
+        return calls.mtla_pages_unpack(self._ptr, cache_c, cache_kr, page_table, packed_cache, first, end, batch, pages_each, stream)
+
+    def decode_attn_packed_status(self, q, q_rope, w_uk, w_uv, cache_c, cache_kr, seq_len, page_table, packed_cache, batch, out,
+                                  out_latent, lse, workspace, stream=None) -> int:
+        return calls.mtla_decode_attn_packed(self._ptr, q, q_rope, w_uk, w_uv, cache_c, cache_kr, seq_len, page_table, packed_cache,
+                                             batch, out, out_latent, lse, workspace, stream)
+
+    def decode_step_packed_status(self, cache_c, cache_kr, tail_c, seq_len, page_table, packed_cache, c_new, kr_new, hyp_A, hyp_a,
+                                  hyp_G, q, q_rope, w_uk, w_uv, batch, out, out_latent, lse, workspace, stream=None) -> int:
+        return calls.mtla_decode_step_packed(self._ptr, cache_c, cache_kr, tail_c, seq_len, page_table, packed_cache, c_new, kr_new,
+                                             hyp_A, hyp_a, hyp_G, q, q_rope, w_uk, w_uv, batch, out, out_latent, lse, workspace,
+                                             stream)
+
+    def packed_codes_bytes(self, n_pages: int) -> int: return lib.mtla_packed_codes_bytes(self._h, n_pages)
+    def packed_scales_bytes(self, n_pages: int) -> int: return lib.mtla_packed_scales_bytes(self._h, n_pages)
+    def packed_keys_bytes(self, n_pages: int) -> int: return lib.mtla_packed_keys_bytes(self._h, n_pages)
+    def pages_fit(self, *a, **k): _check(self.pages_fit_status(*a, **k), "mtla_pages_fit")
+    def pages_pack(self, *a, **k): _check(self.pages_pack_status(*a, **k), "mtla_pages_pack")
+    def pages_unpack(self, *a, **k): _check(self.pages_unpack_status(*a, **k), "mtla_pages_unpack")
+    def decode_attn_packed(self, *a, **k): _check(self.decode_attn_packed_status(*a, **k), "mtla_decode_attn_packed")
+    def decode_step_packed(self, *a, **k): _check(self.decode_step_packed_status(*a, **k), "mtla_decode_step_packed")
 
     def cache_append_paged(self, *a, **k): _check(self.cache_append_paged_status(*a, **k), "mtla_cache_append_paged")
     def decode_attn_paged(self, *a, **k): _check(self.decode_attn_paged_status(*a, **k), "mtla_decode_attn_paged")

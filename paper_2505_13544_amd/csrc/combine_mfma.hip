@@ -307,9 +307,17 @@ __global__ __launch_bounds__((CombineLds<R, DH, RPT, PS>::threads)) void combine
     // lane holds row l16 of the tile, output dims wv * DW + 16nt + 4g .. +3
     const int orow = RPT * t + l16;
     if (l16 < RPT && orow < rows) {
-      float* dst = a.out + ((size_t)orow * a.n_heads + h) * DH + wv * DW + 4 * g;
+      const size_t at = ((size_t)orow * a.n_heads + h) * DH + wv * DW + 4 * g;
+      if (a.out_bf16) {
+        uint16_t* dst = reinterpret_cast<uint16_t*>(a.out) + at;
 #pragma unroll
-      for (int nt = 0; nt < NT; ++nt) *reinterpret_cast<float4_t*>(dst + 16 * nt) = o[nt];
+        for (int nt = 0; nt < NT; ++nt)
+          *reinterpret_cast<uint2*>(dst + 16 * nt) = make_uint2(pack_bf16x2(o[nt][0], o[nt][1]), pack_bf16x2(o[nt][2], o[nt][3]));
+      } else {
+        float* dst = a.out + at;
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) *reinterpret_cast<float4_t*>(dst + 16 * nt) = o[nt];
+      }
     }
     __syncthreads();  // the planes are rewritten by the next tile
   }

@@ -13,6 +13,7 @@
 #include "decode_schedule.h"
 #include "mtla_device.h"
 #include "mtla_kernels.h"
+#include "packed.h"
 
 struct mtla_ctx {
   mtla_config cfg;
@@ -588,6 +589,222 @@ mtla_status mtla_decode_step(mtla_ctx* c, void* cache_c, void* cache_kr, float* 
                              void* workspace, void* hip_stream) {
   return mtla_decode_step_paged(c, cache_c, cache_kr, tail_c, seq_len, nullptr, c_new, kr_new, hyp_A, hyp_a, hyp_G, q, q_rope,
                                 w_uk, w_uv, batch, out, out_latent, lse, workspace, hip_stream);
+}
+
+// ---- packed pages ----------------------------------------------------------------------------------
+// What a packed cache has to have, whoever reads or writes it.
+inline bool packed_cache_ok(const mtla_ctx* c, const mtla_packed_cache* pk) {
+  return pk && pk->codes && pk->scales && pk->keys && pk->table && pk->n_pages >= 1 &&
+         (long long)pk->n_pages * c->cfg.page_slots <= 0x7fffffffLL && aligned16(pk->codes) && aligned16(pk->scales) && aligned16(pk->keys);
+}
+inline PackedMap packed_map(const mtla_packed_cache& pk) {
+  PackedMap m;
+  m.codes = reinterpret_cast<uint8_t*>(pk.codes);
+  m.scales = reinterpret_cast<uint8_t*>(pk.scales);
+  m.keys = reinterpret_cast<uint16_t*>(pk.keys);
+  m.table = pk.table;
+  m.n_packed = pk.n_packed;
+  m.n_pages = pk.n_pages;
+  return m;
+}
+
+size_t mtla_packed_codes_bytes(const mtla_ctx* c, int32_t n_pages) {
+  return c && c->cfg.page_slots > 0 && n_pages > 0 ? (size_t)n_pages * (c->cfg.page_slots / kPackTile) * packed_code_bytes(c->cfg.r) : 0;
+}
+size_t mtla_packed_scales_bytes(const mtla_ctx* c, int32_t n_pages) {
+  return c && c->cfg.page_slots > 0 && n_pages > 0 ? (size_t)n_pages * (c->cfg.page_slots / kPackTile) * packed_scale_bytes(c->cfg.r) : 0;
+}
+size_t mtla_packed_keys_bytes(const mtla_ctx* c, int32_t n_pages) {
+  return c && c->cfg.page_slots > 0 && n_pages > 0 ? (size_t)n_pages * (c->cfg.page_slots / kPackTile) * packed_key_bytes(c->cfg.d_rope) : 0;
+}
+
+static mtla_status pack_args(mtla_ctx* c, const void* cache_c, const void* cache_kr, const int32_t* page_table, const mtla_packed_cache* pk,
+                             const int32_t* first, const int32_t* end, int32_t batch, int32_t pages_each, PackArgs& a) {
+  if (!c || !cache_c || !cache_kr || !page_table || !end) return MTLA_ERR_INVALID_ARG;
+  const mtla_config& g = c->cfg;
+  if (g.page_slots <= 0 || !packed_cache_ok(c, pk)) return MTLA_ERR_INVALID_ARG;
+  if (batch < 1 || batch > g.max_batch || pages_each < 0) return MTLA_ERR_INVALID_ARG;
+  if (!aligned16(cache_c) || !aligned16(cache_kr)) return MTLA_ERR_INVALID_ARG;
+  a.cache_c = const_cast<void*>(cache_c);
+  a.cache_kr = const_cast<void*>(cache_kr);
+  a.pages = page_map(c, page_table);
+  a.pk = packed_map(*pk);
+  a.first = first;
+  a.end = end;
+  a.batch = batch;
+  a.r = g.r;
+  a.d_rope = g.d_rope;
+  a.pages_each = pages_each;
+  return MTLA_OK;
+}
+
+mtla_status mtla_pages_pack(mtla_ctx* c, const void* cache_c, const void* cache_kr, const int32_t* page_table, const mtla_packed_cache* pk,
+                            const int32_t* first, const int32_t* end, int32_t batch, int32_t pages_each, void* hip_stream) {
+  PackArgs a;
+  const mtla_status ok = pack_args(c, cache_c, cache_kr, page_table, pk, first, end, batch, pages_each, a);
+  if (ok != MTLA_OK) return ok;
+  return hip_ok(launch_pack(a, reinterpret_cast<hipStream_t>(hip_stream))) ? MTLA_OK : MTLA_ERR_HIP;
+}
+
+mtla_status mtla_pages_unpack(mtla_ctx* c, void* cache_c, void* cache_kr, const int32_t* page_table, const mtla_packed_cache* pk,
+                              const int32_t* first, const int32_t* end, int32_t batch, int32_t pages_each, void* hip_stream) {
+  PackArgs a;
+  const mtla_status ok = pack_args(c, cache_c, cache_kr, page_table, pk, first, end, batch, pages_each, a);
+  if (ok != MTLA_OK) return ok;
+  return hip_ok(launch_unpack(a, reinterpret_cast<hipStream_t>(hip_stream))) ? MTLA_OK : MTLA_ERR_HIP;
+}
+
+inline bool fit_pool(const mtla_page_pool* p, int page_slots, FitPool& out) {
+  if (!p || !p->table || !p->first || !p->end || !p->ring || !p->state || p->n_pages < 1 || p->spill >= p->n_pages) return false;
+  if ((long long)p->n_pages * page_slots > 0x7fffffffLL) return false;
+  out.table = p->table;
+  out.first = p->first;
+  out.end = p->end;
+  out.ring = p->ring;
+  out.state = p->state;
+  out.was_end = p->was_end;
+  out.n_pages = p->n_pages;
+  out.spill = p->spill;
+  return true;
+}
+
+mtla_status mtla_pages_fit(mtla_ctx* c, const mtla_page_pool* pool, const mtla_page_pool* packed, const int32_t* seq_len, const int32_t* n_new,
+                           int32_t n_new_max, int32_t keep_pages, int32_t batch, int64_t* slot_map, void* workspace, void* hip_stream) {
+  if (!c || !seq_len || !workspace) return MTLA_ERR_INVALID_ARG;
+  const mtla_config& g = c->cfg;
+  if (g.page_slots <= 0 || batch < 1 || batch > g.max_batch || n_new_max < 0 || keep_pages < 0) return MTLA_ERR_INVALID_ARG;
+  if (slot_map && n_new_max < 1) return MTLA_ERR_INVALID_ARG;
+  FitArgs a;
+  if (!fit_pool(pool, g.page_slots, a.pool) || (packed && !fit_pool(packed, g.page_slots, a.packed))) return MTLA_ERR_INVALID_ARG;
+  if (packed && (packed->table == pool->table || packed->first == pool->first || packed->end == pool->end || packed->ring == pool->ring ||
+                 packed->state == pool->state))
+    return MTLA_ERR_INVALID_ARG;
+  a.seq_len = seq_len;
+  a.n_new = n_new;
+  a.slot_map = slot_map;
+  a.status = reinterpret_cast<int32_t*>(workspace);
+  a.n_new_max = n_new_max;
+  a.keep_pages = keep_pages;
+  a.batch = batch;
+  a.max_pages = max_pages(g);
+  a.stride = g.stride;
+  a.max_slots = g.max_slots;
+  a.shift = page_map(c, pool->table).shift;
+  return hip_ok(launch_pages_fit(a, reinterpret_cast<hipStream_t>(hip_stream))) ? MTLA_OK : MTLA_ERR_HIP;
+}
+
+// Attention of one decode step over packed pages; `ap` (may be NULL) is the append in front of it.
+static mtla_status decode_packed_core(mtla_ctx* c, const AppendArgs* ap, const void* q, const void* q_rope, const void* w_uk, const void* w_uv,
+                                      const void* cache_c, const void* cache_kr, const int32_t* seq_len, const int32_t* page_table,
+                                      const mtla_packed_cache* pk, int32_t batch, void* out, float* out_latent, float* lse, void* workspace,
+                                      void* hip_stream) {
+  if (!c || !q || !q_rope || !w_uk || !cache_c || !cache_kr || !seq_len || !page_table || !workspace) return MTLA_ERR_INVALID_ARG;
+  const mtla_config& g = c->cfg;
+  if (!paging_matches(c, page_table) || !packed_cache_ok(c, pk) || !pk->n_packed) return MTLA_ERR_INVALID_ARG;
+  if (batch < 1 || batch > g.max_batch) return MTLA_ERR_INVALID_ARG;
+  if ((out != nullptr) != (w_uv != nullptr)) return MTLA_ERR_INVALID_ARG;
+  if (!out && !out_latent && !lse) return MTLA_ERR_INVALID_ARG;
+  if (!aligned16(q) || !aligned16(q_rope) || !aligned16(w_uk) || !aligned16(cache_c) || !aligned16(cache_kr) || !aligned16(workspace) ||
+      (w_uv && !aligned16(w_uv)))
+    return MTLA_ERR_INVALID_ARG;
+  if (c->prefix_owner) return MTLA_ERR_UNSUPPORTED;  // with pages a shared prompt is shared pages
+  hipStream_t st = reinterpret_cast<hipStream_t>(hip_stream);
+  char* ws = reinterpret_cast<char*>(workspace);
+  const DecodeLayout L = decode_layout(c);
+
+  AbsorbArgs ab;
+  ab.q = q;
+  ab.q_rope = q_rope;
+  ab.w_uk = w_uk;
+  ab.qcat = ws + L.qcat;
+  ab.rows = batch;
+  ab.n_heads = g.n_heads;
+  ab.d_head = g.d_head;
+  ab.r = g.r;
+  ab.d_rope = g.d_rope;
+  ab.scale_log2 = c->scale * 1.4426950408889634f;
+  ab.q_f32 = 0;
+  ab.out_bf16 = 1;
+  ab.plane = (size_t)g.max_batch * g.n_heads * (g.r + g.d_rope);
+
+  CombineArgs cb;
+  cb.part_o = reinterpret_cast<float*>(ws + L.part_o);
+  cb.part_ml = reinterpret_cast<float*>(ws + L.part_ml);
+  cb.seq_len = seq_len;
+  cb.w_uv = w_uv;
+  cb.out = reinterpret_cast<float*>(out);
+  cb.out_bf16 = 1;
+  cb.out_latent = out_latent;
+  cb.lse = lse;
+  cb.n_heads = g.n_heads;
+  cb.r = g.r;
+  cb.d_head = g.d_head;
+  cb.stride = g.stride;
+  cb.max_slots = g.max_slots;
+  cb.chunk = c->chunk;
+  cb.n_splits = n_splits(c);
+  cb.batch = batch;
+  cb.T = 0;
+  cb.n_persistent = 0;
+  cb.tile_prefix = nullptr;
+  cb.part_f16 = combine_mfma_supported(cb) ? 1 : 0;
+
+  AttnPackedArgs a;
+  AttnArgs& at = a.at;
+  at.qcat = ab.qcat;
+  at.q_plane = ab.plane;
+  at.lat = cache_c;
+  at.key = cache_kr;
+  at.seq_len = seq_len;
+  at.part_o = reinterpret_cast<float*>(ws + L.part_o);
+  at.part_ml = reinterpret_cast<float*>(ws + L.part_ml);
+  at.n_heads = g.n_heads;
+  at.r = g.r;
+  at.d_rope = g.d_rope;
+  at.stride = g.stride;
+  at.max_slots = g.max_slots;
+  at.chunk = cb.chunk;
+  at.n_splits = cb.n_splits;
+  at.batch = batch;
+  at.T = 0;
+  at.n_persistent = 0;
+  at.tile_prefix = nullptr;
+  at.part_f16 = cb.part_f16;
+  at.pages = page_map(c, page_table);
+  a.pk = packed_map(*pk);
+
+  EventPair ev;
+  if (c->prof_n < (int)c->ev_start.size()) {
+    ev.start = c->ev_start[c->prof_n];
+    ev.stop = c->ev_stop[c->prof_n++];
+  }
+  if (ap && decode_front_supported(*ap, ab)) {
+    if (!hip_ok(launch_decode_front(*ap, ab, st))) return MTLA_ERR_HIP;
+  } else {
+    if (ap && !hip_ok(launch_append(*ap, g.dtype, st))) return MTLA_ERR_HIP;
+    if (!hip_ok(launch_absorb(ab, g.dtype, st))) return MTLA_ERR_HIP;
+  }
+  if (!hip_ok(launch_attn_packed(a, st, ev))) return MTLA_ERR_HIP;
+  return hip_ok(launch_combine(cb, g.dtype, st)) ? MTLA_OK : MTLA_ERR_HIP;
+}
+
+mtla_status mtla_decode_attn_packed(mtla_ctx* c, const void* q, const void* q_rope, const void* w_uk, const void* w_uv, const void* cache_c,
+                                    const void* cache_kr, const int32_t* seq_len, const int32_t* page_table, const mtla_packed_cache* pk,
+                                    int32_t batch, void* out, float* out_latent, float* lse, void* workspace, void* hip_stream) {
+  return decode_packed_core(c, nullptr, q, q_rope, w_uk, w_uv, cache_c, cache_kr, seq_len, page_table, pk, batch, out, out_latent, lse, workspace,
+                            hip_stream);
+}
+
+mtla_status mtla_decode_step_packed(mtla_ctx* c, void* cache_c, void* cache_kr, float* tail_c, int32_t* seq_len, const int32_t* page_table,
+                                    const mtla_packed_cache* pk, const void* c_new, const void* kr_new, const void* hyp_A, const void* hyp_a,
+                                    const void* hyp_G, const void* q, const void* q_rope, const void* w_uk, const void* w_uv, int32_t batch, void* out,
+                                    float* out_latent, float* lse, void* workspace, void* hip_stream) {
+  AppendArgs ap;
+  const mtla_status ok = append_args(c, cache_c, cache_kr, tail_c, seq_len, c_new, kr_new, nullptr, 1, batch, hyp_A, hyp_a, hyp_G, nullptr, nullptr,
+                                     nullptr, workspace, ap, page_table);
+  if (ok != MTLA_OK) return ok;
+  return decode_packed_core(c, &ap, q, q_rope, w_uk, w_uv, cache_c, cache_kr, seq_len, page_table, pk, batch, out, out_latent, lse, workspace,
+                            hip_stream);
 }
 
 // Beam search over paged storage: destination b continues source src_index[b].  Its table row takes the

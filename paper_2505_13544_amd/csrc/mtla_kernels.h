@@ -76,6 +76,17 @@ struct AttnArgs {
   PageMap pages;         // decode, matrix-core kernels only: paged storage of lat / key (table NULL: contiguous)
 };
 
+// Complete pages in 4 bits (packed.h): logical pages 0 .. n_packed[b] - 1 of sequence b live in page table[b * max_pages + k] of
+// these arrays, the ones behind them in the bf16 pool.
+struct PackedMap {
+  uint8_t* codes = nullptr;
+  uint8_t* scales = nullptr;
+  uint16_t* keys = nullptr;
+  const int32_t* table = nullptr;     // device, [batch rows, max_pages]
+  const int32_t* n_packed = nullptr;  // device, [batch]; taken as [0, max_pages]
+  int n_pages = 0;                    // a table entry is clamped into [0, n_pages)
+};
+
 // Decode kernels: a sequence whose first n slots are read from another sequence's rows of the same
 // arrays (a prompt stored once for all beams); those rows lie dlat / dkey elements away from its own.
 struct SharedPrefix {
@@ -119,6 +130,7 @@ struct CombineArgs {
   const int32_t* tile_prefix;   // balanced: [batch + 1] running work units
   int run_cost = 0;             // balanced: units before a row's first tile (as the attention kernel counted)
   int part_f16;                 // part_o holds normalised IEEE-half partials (matrix-core combine only)
+  int out_bf16 = 0;             // out is bf16 [rows, n_heads, d_head]
 };
 
 // Decode attention and value up-projection of whole sequences in one launch (attn_whole.hip).
@@ -306,6 +318,43 @@ struct ForkArgs {
   int batch, max_batch, max_slots, stride, r, d_rope;
 };
 
+// Decode attention over packed pages and, behind them, pages of the bf16 pool (attn_packed.hip).
+struct AttnPackedArgs {
+  AttnArgs at;   // lat, key: the bf16 pool; pages: its table
+  PackedMap pk;
+};
+
+// Pages first[b] .. end[b] - 1 of every sequence between the bf16 pool and packed pages (pages_pack.hip).
+struct PackArgs {
+  void* cache_c;             // the bf16 pool
+  void* cache_kr;
+  PageMap pages;             // its table
+  PackedMap pk;              // (n_packed is not looked at)
+  const int32_t* first;      // [batch] or NULL: 0
+  const int32_t* end;        // [batch]
+  int batch, r, d_rope, pages_each;
+};
+
+// Pools whose tables are made to fit the sequences' lengths (pages_fit.hip).
+struct FitPool {
+  int32_t* table = nullptr;   // [max_batch, max_pages]
+  int32_t* first = nullptr;   // [max_batch] entries first .. end - 1 of a row name pages that the sequence holds
+  int32_t* end = nullptr;
+  int32_t* ring = nullptr;    // [n_pages] free pages: `count` from place `head` on, wrapping round
+  int32_t* state = nullptr;   // [4]: head, count, sequences refused by the last call, 0
+  int32_t* was_end = nullptr; // [max_batch] or NULL: `end` as it was before the call
+  int n_pages = 0;
+  int spill = -1;             // page that the entries of a refused sequence name; below 0: they are left alone
+};
+struct FitArgs {
+  FitPool pool, packed;       // packed.table NULL: one pool
+  const int32_t* seq_len;     // [batch]
+  const int32_t* n_new;       // [batch] or NULL: n_new_max
+  int64_t* slot_map;          // [batch, n_new_max] or NULL
+  int32_t* status;            // workspace header word
+  int n_new_max, keep_pages, batch, max_pages, stride, max_slots, shift;
+};
+
 // Projections in front of and behind the decode path (bf16), one token per sequence.
 struct LayerFrontArgs {
   const void* x;       // [batch, d_model]
@@ -417,6 +466,11 @@ hipError_t launch_gemm_ring(const GemmArgs& a, hipStream_t st);
 // the same products as streams of 256 x 256 tiles (launch_gemm_nt picks)
 bool gemm_wide_supported(const GemmArgs& a);
 hipError_t launch_gemm_wide(const GemmArgs& a, hipStream_t st);
+// packed pages: attention over them (static schedule; heads of more than two tiles by a grid dimension), the pages' ways in and out, and the tables
+hipError_t launch_attn_packed(const AttnPackedArgs& a, hipStream_t st, const EventPair& ev = EventPair());
+hipError_t launch_pack(const PackArgs& a, hipStream_t st);
+hipError_t launch_unpack(const PackArgs& a, hipStream_t st);
+hipError_t launch_pages_fit(const FitArgs& a, hipStream_t st);
 hipError_t launch_combine(const CombineArgs& a, int dtype, hipStream_t st);
 bool combine_mfma_supported(const CombineArgs& a);  // bf16 storage; r, d_head and alignment fit
 hipError_t launch_combine_mfma(const CombineArgs& a, hipStream_t st);

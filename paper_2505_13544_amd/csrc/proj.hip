@@ -131,6 +131,11 @@ __host__ __device__ inline int lanes_per_out_col(int dh) {  // power of two, kBl
   return t >= 8 ? 8 : (t >= 4 ? 4 : (t >= 2 ? 2 : 1));
 }
 
+__device__ __forceinline__ void store_out(const CombineArgs& a, size_t at, float v) {
+  if (a.out_bf16) reinterpret_cast<uint16_t*>(a.out)[at] = f32_to_bf16_bits(v);
+  else a.out[at] = v;
+}
+
 template <typename T, int NCH, bool INLINE>
 __global__ __launch_bounds__(kBlock) void combine_kernel(CombineArgs a) {
   extern __shared__ float smem[];
@@ -197,7 +202,7 @@ __global__ __launch_bounds__(kBlock) void combine_kernel(CombineArgs a) {
     if (a.out_latent)
       for (int n = tid; n < r; n += kBlock) a.out_latent[oh * r + n] = 0.f;
     if (a.out)
-      for (int dd = tid; dd < dh; dd += kBlock) a.out[oh * dh + dd] = 0.f;
+      for (int dd = tid; dd < dh; dd += kBlock) store_out(a, oh * dh + dd, 0.f);
     if (a.lse && tid == 0) a.lse[oh] = -INFINITY;
     return;
   }
@@ -291,7 +296,7 @@ __global__ __launch_bounds__(kBlock) void combine_kernel(CombineArgs a) {
     }
   }
   for (int off = 1; off < tpd; off <<= 1) part += __shfl_xor(part, off, kWave);
-  if (d < dh && qd == 0) a.out[oh * dh + d] = part;
+  if (d < dh && qd == 0) store_out(a, oh * dh + d, part);
 }
 
 template <typename T, bool INLINE>

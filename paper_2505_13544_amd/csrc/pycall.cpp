@@ -4,7 +4,7 @@
 // ctypes took 8 us of host time a call, more than the GPU needs for the step of a small model; here the same call costs
 // under 1 us.  A pointer argument is a tensor, an integer address, None (NULL) or any object with data_ptr().  Nothing else
 // is one: most pointers are device memory, and host memory taken for it (a numpy array, a bytes object) would be read by a
-// kernel.  Only a page book, which the library's host functions read, is a writable buffer (the ctypes structure).  The
+// kernel.  Only a page book, a page pool and a packed cache, structures in host memory, are writable buffers (the ctypes structures).  The
 // argument types come from the declarations in mtla.h.  The addresses of the functions are handed in by the binding
 // (bind), which has loaded the library: this module does not link against it.
 #define PY_SSIZE_T_CLEAN
@@ -24,10 +24,11 @@ namespace {
 // What a call needs beyond its C arguments: storage for structures built from dicts, buffers to release.
 struct Hold {
   mtla_layer_weights lw;
-  Py_buffer view;
-  bool has_view = false;
+  static constexpr int kViews = 2;  // structures of one call (the two pools of mtla_pages_fit)
+  Py_buffer view[kViews];
+  int n_views = 0;
   ~Hold() {
-    if (has_view) PyBuffer_Release(&view);
+    for (int i = 0; i < n_views; ++i) PyBuffer_Release(&view[i]);
   }
 };
 
@@ -57,17 +58,18 @@ bool structure(PyObject* o, size_t bytes, Hold& hold, void*& out) {
     out = nullptr;
     return true;
   }
-  if (hold.has_view) {
-    PyErr_SetString(PyExc_TypeError, "more than one structure argument");
+  if (hold.n_views == Hold::kViews) {
+    PyErr_SetString(PyExc_TypeError, "too many structure arguments");
     return false;
   }
-  if (PyObject_GetBuffer(o, &hold.view, PyBUF_WRITABLE) != 0) return false;
-  hold.has_view = true;
-  if ((size_t)hold.view.len != bytes) {
-    PyErr_Format(PyExc_TypeError, "a structure of %zu bytes is needed, the buffer has %zd", bytes, hold.view.len);
+  Py_buffer& view = hold.view[hold.n_views];
+  if (PyObject_GetBuffer(o, &view, PyBUF_WRITABLE) != 0) return false;
+  ++hold.n_views;
+  if ((size_t)view.len != bytes) {
+    PyErr_Format(PyExc_TypeError, "a structure of %zu bytes is needed, the buffer has %zd", bytes, view.len);
     return false;
   }
-  out = hold.view.buf;
+  out = view.buf;
   return true;
 }
 
@@ -115,6 +117,9 @@ bool layer_weights(PyObject* d, mtla_layer_weights& w) {
 }
 
 template <class T>
+constexpr bool is_structure = std::is_same_v<T, mtla_page_book> || std::is_same_v<T, mtla_page_pool> || std::is_same_v<T, mtla_packed_cache>;
+
+template <class T>
 bool convert(PyObject* o, Hold& hold, T& out) {
   if constexpr (std::is_pointer_v<T>) {
     if constexpr (std::is_same_v<T, const mtla_layer_weights*>) {
@@ -122,7 +127,9 @@ bool convert(PyObject* o, Hold& hold, T& out) {
       out = &hold.lw;
     } else {
       void* p;
-      const bool ok = std::is_same_v<T, mtla_page_book*> ? structure(o, sizeof(mtla_page_book), hold, p) : address(o, p);
+      bool ok;
+      if constexpr (is_structure<std::remove_const_t<std::remove_pointer_t<T>>>) ok = structure(o, sizeof(std::remove_pointer_t<T>), hold, p);
+      else ok = address(o, p);
       if (!ok) return false;
       out = reinterpret_cast<T>(p);
     }
@@ -165,7 +172,8 @@ PyObject* invoke(R (*fn)(A...), PyObject* const* args, Py_ssize_t n, const char*
   X(mtla_cache_append) X(mtla_decode_attn) X(mtla_decode_step) X(mtla_decode_step_static) X(mtla_cache_append_paged) \
   X(mtla_decode_attn_paged) X(mtla_decode_step_paged) X(mtla_prefill_chunk_attn_paged) X(mtla_prefill_step_paged)    \
   X(mtla_cache_fork_paged) X(mtla_prefill_attn) X(mtla_prefill_chunk_attn) X(mtla_prefill_step) X(mtla_cache_reorder) \
-  X(mtla_cache_reorder_from) X(mtla_layer_decode_step) X(mtla_layer_prefill) X(mtla_pages_reserve) X(mtla_pages_fork)
+  X(mtla_cache_reorder_from) X(mtla_layer_decode_step) X(mtla_layer_prefill) X(mtla_pages_reserve) X(mtla_pages_fork) \
+  X(mtla_pages_fit) X(mtla_pages_pack) X(mtla_pages_unpack) X(mtla_decode_attn_packed) X(mtla_decode_step_packed)
 
 #define DEFINE(NAME)                                                                                            \
   decltype(&NAME) p_##NAME = nullptr;                                                                           \

@@ -420,3 +420,131 @@ class PagedSession:
 
     def device_status(self) -> int:
         return self.ctx.device_status(self.workspace, self.stream)
+
+
+class PackedSession:
+    """Session over paged slot storage whose complete pages are held in 4 bits, with the page tables kept on the device: no call needs
+    the lengths on the host, so whole steps, pages changing hands among them, can be captured into a graph and replayed.
+
+    A step is fit (tables follow the lengths), pack (pages completed since go into packed pages, their bf16 pages go back to the pool) and the
+    decode step over both kinds of page.  `n_pages` bounds the bf16 pages (per sequence: the ones being written to, the newest `keep_pages` complete
+    ones, and one that is between two steps; whole prompts while their prefill runs), `n_packed_pages` the packed ones.  One more bf16 page than
+    that is allocated: what a sequence without a page appends goes there (device_status() then says MTLA_ERR_CAPACITY, refused() how many)."""
+
+    def __init__(self, *, n_heads, d_head, r, d_rope, d_hyper, stride, max_batch, max_slots, page_slots, n_pages, n_packed_pages,
+                 keep_pages: int = 0, softmax_scale: float = 0.0, device="cuda:0", decode_chunk: Optional[int] = None, page_order=None):
+        if not torch.cuda.is_available():
+            raise RuntimeError("libmtla needs a GPU: no HIP device is visible")
+        if keep_pages < 0:
+            raise ValueError("keep_pages is a number of pages")
+        self.dtype, self.device, self.tdt = "bf16", torch.device(device), torch.bfloat16
+        self.ctx = B.Context(n_heads=n_heads, d_head=d_head, r=r, d_rope=d_rope, d_hyper=d_hyper, stride=stride, max_batch=max_batch,
+                             max_slots=max_slots, dtype="bf16", softmax_scale=softmax_scale, page_slots=page_slots, n_pages=n_pages + 1)
+        if decode_chunk:
+            self.ctx.set_decode_chunk(decode_chunk)
+        self.n_heads, self.d_head, self.r, self.d_rope = n_heads, d_head, r, d_rope
+        self.stride, self.max_batch, self.max_slots, self.page_slots, self.keep_pages = stride, max_batch, max_slots, page_slots, keep_pages
+        self.max_pages = -(-max_slots // page_slots)
+        dev, tiles = self.device, page_slots // 16
+        ints = lambda *shape: torch.zeros(*shape, dtype=torch.int32, device=dev)
+        self.pool_c = torch.zeros(n_pages + 1, page_slots, r, dtype=self.tdt, device=dev)
+        self.pool_kr = torch.zeros(n_pages + 1, page_slots, d_rope, dtype=self.tdt, device=dev)
+        self.codes = torch.zeros(n_packed_pages, tiles, r // 32, 16, 16, dtype=torch.uint8, device=dev)
+        self.scales = torch.zeros(n_packed_pages, tiles, r // 32, 16, dtype=torch.uint8, device=dev)
+        self.keys = torch.zeros(n_packed_pages, tiles, d_rope // 8, 16, 8, dtype=self.tdt, device=dev)
+        assert self.codes.numel() == self.ctx.packed_codes_bytes(n_packed_pages)
+        assert self.scales.numel() == self.ctx.packed_scales_bytes(n_packed_pages)
+        assert self.keys.numel() * 2 == self.ctx.packed_keys_bytes(n_packed_pages)
+        order = torch.arange(n_pages) if page_order is None else torch.as_tensor(np.ascontiguousarray(page_order))
+        order4 = torch.arange(n_packed_pages)
+
+        def pool(ring, spill):
+            return B.PagePool(ints(max_batch, self.max_pages), ints(max_batch), ints(max_batch), ring.to(torch.int32).to(dev),
+                              torch.tensor([0, ring.numel(), 0, 0], dtype=torch.int32, device=dev), was_end=ints(max_batch), spill=spill)
+
+        # (the ring of the bf16 pool has a place for every page of the pool, the spill page is in none of them)
+        self.pool = pool(torch.cat([order, torch.full((1,), n_pages)]), n_pages)
+        self.pool.tensors["state"][1] = n_pages
+        self.packed = pool(order4, -1)
+        self.table = self.pool.tensors["table"]
+        self.cache = B.PackedCache(self.codes, self.scales, self.keys, self.packed.tensors["table"], self.packed.tensors["end"])
+        self.tail_c = torch.zeros(max_batch, r, dtype=torch.float32, device=dev)
+        self.seq_len = ints(max_batch)
+        self.workspace = torch.empty(self.ctx.workspace_bytes(), dtype=torch.uint8, device=dev)
+        self.ctx.workspace_init(self.workspace, self.stream)
+        self.hyp_A = self.hyp_a = self.hyp_G = self.w_uk = self.w_uv = None
+
+    @property
+    def stream(self) -> int:
+        return _raw_stream(self.device)
+
+    set_weights = Session.set_weights
+
+    # ---- pages
+    def _part(self, at: int):
+        """Tables and state of the sequences from `at` on: (pool, packed pool, packed cache)."""
+        if at == 0:
+            return self.pool, self.packed, self.cache
+        if not 0 < at < self.max_batch:
+            raise IndexError(f"sequence {at} of a session of {self.max_batch}")
+
+        def part(p):
+            t = p.tensors
+            return B.PagePool(t["table"][at:], t["first"][at:], t["end"][at:], t["ring"], t["state"], t["was_end"][at:], p.spill)
+
+        pool, packed = part(self.pool), part(self.packed)
+        return pool, packed, B.PackedCache(self.codes, self.scales, self.keys, packed.tensors["table"], packed.tensors["end"])
+
+    def fit(self, batch: int, n_new: int = 0, *, counts=None, slot_map=None, at: int = 0):
+        """Tables of sequences at .. at + batch - 1 for n_new more tokens (counts: an int32 device tensor of how many of them, per
+        sequence); pages completed since the last call are packed."""
+        pool, packed, cache = self._part(at)
+        self.ctx.pages_fit(pool, packed, self.seq_len[at:], counts, n_new, self.keep_pages, batch, slot_map, self.workspace, self.stream)
+        t = packed.tensors
+        self.ctx.pages_pack(self.pool_c, self.pool_kr, pool.tensors["table"], cache, t["was_end"], t["end"], batch, 1, self.stream)
+
+    def unpack(self, batch: int, n_new: int = 0, *, counts=None, slot_map=None, at: int = 0):
+        """The sequences in bf16 pages alone, with room for n_new more tokens: what a prefill that continues them reads.  Their packed pages
+        stay as they are; the next fit gives the bf16 ones back."""
+        pool, packed, cache = self._part(at)
+        self.ctx.pages_fit(pool, None, self.seq_len[at:], counts, n_new, 0, batch, slot_map, self.workspace, self.stream)
+        # (a sequence that got no pages holds none below its first: none of another's is written)
+        self.ctx.pages_unpack(self.pool_c, self.pool_kr, pool.tensors["table"], cache, pool.tensors["first"], packed.tensors["end"], batch,
+                              self.max_pages, self.stream)
+
+    def release(self, rows):
+        """The sequences `rows` (an index of any kind) are done: empty from here on, their pages go back with the next fit."""
+        self.seq_len[rows] = 0
+
+    def refused(self):
+        """Sequences that the last fit had no page for, in the bf16 pool and in the packed one."""
+        return int(self.pool.tensors["state"][2]), int(self.packed.tensors["state"][2])
+
+    # ---- calls
+    def prefill(self, q, q_rope, c, kr, *, out, max_past_slots: int = 0, n_new=None, w_out=None, at: int = 0):
+        """T tokens for sequences at .. at + c.shape[0] - 1, empty ones or ones that continue (`max_past_slots` bounds their slots);
+        n_new: int32 device tensor or None for all.  The prompts' complete pages are packed behind it."""
+        batch, T = c.shape[0], c.shape[1]
+        self.unpack(batch, T, counts=n_new, at=at)
+        scratch = torch.empty(self.ctx.prefill_step_scratch_bytes(batch, T, max_past_slots), dtype=torch.uint8, device=self.device)
+        self.ctx.prefill_step_paged(self.pool_c, self.pool_kr, self.tail_c[at:], self.seq_len[at:], self.table[at:], q, q_rope, c, kr, n_new,
+                                    self.hyp_A, self.hyp_a, self.hyp_G, self.w_uk, self.w_uv, batch, T, max_past_slots, out, w_out,
+                                    scratch, self.workspace, self.stream)
+        self.fit(batch, at=at)
+        return scratch  # keep alive until the stream has consumed it
+
+    def decode(self, q, q_rope, *, out=None, out_latent=None, lse=None):
+        """One query per sequence; out is bf16."""
+        self.ctx.decode_attn_packed(q, q_rope, self.w_uk, self.w_uv if out is not None else None, self.pool_c, self.pool_kr, self.seq_len,
+                                    self.table, self.cache, q.shape[0], out, out_latent, lse, self.workspace, self.stream)
+
+    def step(self, c_new, kr_new, q, q_rope, *, out=None, out_latent=None, lse=None):
+        """One step of incremental inference: tables, packing, the append of every sequence's token, attention; out is bf16."""
+        batch = len(q)
+        self.fit(batch, 1)
+        self.ctx.decode_step_packed(self.pool_c, self.pool_kr, self.tail_c, self.seq_len, self.table, self.cache, c_new, kr_new, self.hyp_A,
+                                    self.hyp_a, self.hyp_G, q, q_rope, self.w_uk, self.w_uv if out is not None else None, batch, out,
+                                    out_latent, lse, self.workspace, self.stream)
+
+    def device_status(self) -> int:
+        return self.ctx.device_status(self.workspace, self.stream)
