@@ -1,83 +1,118 @@
 // Decode attention over packed pages (packed.h) and, behind them, pages of the bf16 pool (gfx950).
 //
-// Eq. (with-rope), incremental case, per 32 slots and 16 heads:
+// Eq. (with-rope), incremental case, per tile of 16 slots and 16 heads:
 //     S^T[slot, head] = [C_hat | K_hat^R][slot, :] . [q~ | q^R][head, :]
 //     O^T[col,  head] += C_hat^T[col, slot] . P^T[slot, head]
-// Workgroup = (chunk of slots, sequence); wavefront w owns latent columns [w r/4, (w+1) r/4) and a quarter of the RoPE columns, as in the column-split
-// kernel for bf16 rows: every byte of the cache is loaded once whatever the number of heads, the wavefronts' shares of S^T meet in LDS, all form the same
-// weights, and each ends with its own columns of the sums.  A lane loads the codes of r / 16 latents of one slot (at r = 512 a whole block of
-// 32 with its scale), turns them into bf16 (exact: packed.h) and has them in the A operand's layout of v_mfma_f32_16x16x32_bf16 at once: the order
-// of a contraction's terms is free, so the query is brought into the order in which the codes lie.  The same registers go through LDS and
-// come back transposed for the value product.
-// The query comes as two bf16 planes (hi + lo), and so do the weights here: the packed cache is a third of the bytes of the bf16 one, the matrix cores have
-// time for the second product, and the output's error is its own rounding to bf16 (one plane of weights would add as much again).
-// The normaliser sums the unrounded weights.
+// Workgroup = (sequence, 16 heads, chunk of slots).  A wavefront owns 128 latent columns (all 64 at r = 64): CG = r / 128 of them share the slots of a step
+// (64 at r = 512, else 32), and the 4 / CG groups take different slots.  Every byte of the cache is loaded once per 16 heads.
+//   logits   the codes go into the matrix cores as they are: v_mfma_scale_f32_16x16x128_f8f6f4 takes a lane's 32 codes of a slot with the block's power of
+//            two, against the query as four planes of 6-bit floats (E2M3), each with a power of two per 32 columns of a head.  Plane after plane takes what
+//            the ones before left: off by 2^-18 of the block's largest number after four (QueryPlanes).  64 cycles a tile, against 128 for two bf16 planes
+//            behind a conversion of the codes.  The RoPE columns are bf16 on either side (two planes of the query).
+//   weights  the group's shares of S^T meet in LDS; every wavefront makes the weights of its own tiles, as two bf16 planes, which all read.
+//   values   the codes go through the wavefront's own LDS as they are and come back transposed by bytes; behind that they become bf16 pairs and operands.
+//            Converted first, as bf16 rows, they were four times the bytes there: of a step's 1900 cycles LDS was busy with 960 (13 a 16-byte store of a wavefront).
+// The packed cache is a third of the bytes of the bf16 one, so the matrix cores have time for the second plane of the weights: the output's error is its own
+// rounding to bf16 (one plane would add as much again).  The normaliser sums the unrounded weights.
+//
+// Between two barriers a wavefront forms the values of step i - 1, the weights of step i and the logits of step i + 1.  What bounds it, r = 512, 16 heads:
+//   512 x 1024 slots (two workgroups a unit)  53 us, 4.0 TB/s: half the time VALU, a quarter MFMA, and the memory (47 us with all pages in L2)
+//   256 x 1024 slots (one)                    32 us, 3.3 TB/s: what a step waits for, one after the other (0.7 us for 32 slots)
+//   256 x 32 slots                            10 us: the launch and three reads that wait for each other
+// An equal share of all steps for each of 512 workgroups took 47 us instead of 49 where 256 lengths range from 256 to 2048 slots, and 37 instead of 32 where all are
+// 1024: its scan of the lengths is one more read to wait for.
 #include "bounds.h"
 #include "lds_stream.h"
 #include "mtla_device.h"
 #include "packed.h"
+
+#include <type_traits>
 
 namespace mtla {
 
 namespace {
 
 typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
+typedef short short8_t __attribute__((ext_vector_type(8)));
+typedef int i32x8_t __attribute__((ext_vector_type(8)));
+typedef int i32x2_t __attribute__((ext_vector_type(2)));
+typedef __attribute__((address_space(3))) i32x2_t* lds_int2_ptr;
+typedef uint32_t u32x6_t __attribute__((ext_vector_type(6)));
+typedef float f32x16_t __attribute__((ext_vector_type(16)));
+typedef float f32x32_t __attribute__((ext_vector_type(32)));
 
 constexpr int kWaves = kBlock / kWave;
 constexpr int kTile = kPackTile;   // slots of an operand tile
-constexpr int kStep = 2 * kTile;   // slots of a step: the contraction of the value product
+constexpr float kRebase = 40.f;
 
-template <int R_, int DR_, int NHT_>
+template <int R_, int DR_>
 struct PackCfg {
-  static constexpr int R = R_, DR = DR_, NHT = NHT_;
+  static constexpr int R = R_, DR = DR_;
   static constexpr int E = R + DR;
-  static constexpr int RW = R / kWaves;               // latent columns of a wavefront
-  static constexpr bool kMixed = RW < 32;             // r = 64: one K step holds the latents (lanes g < 2) and the RoPE columns
-  static constexpr int LN = kMixed ? 8 : RW / 4;      // latent columns of a lane
-  static constexpr int KC = kMixed ? 0 : RW / 32;     // K steps of latents alone
-  static constexpr int KQ = KC + 1;                   // and the one with the RoPE columns (lanes without any hold zeros)
-  static constexpr int DRW = DR / kWaves;             // RoPE columns of a wavefront: 8 or 16
+  static constexpr int CG = R >= 128 ? R / 128 : 1;   // wavefronts that share a group's slots
+  static constexpr int SG = kWaves / CG;              // groups
+  static constexpr int RW = R / CG;                   // latent columns of a wavefront: 128, or 64
+  static constexpr int NB = RW / kPackBlock;          // blocks of a slot: one in each of the lanes g < NB
+  static constexpr int DRW = DR / CG;                 // RoPE columns of a wavefront: 8 to 64
+  static constexpr int KR = (DRW + 31) / 32;          // K steps over them
   static constexpr int MT = RW / 16;                  // column tiles of its sums
-  static constexpr int TS = RW + 16;                  // row stride of the parked slice
-  static constexpr int CW = LN / 8;                   // words of codes of a lane
-  static constexpr size_t park_bytes = (size_t)kWaves * kStep * TS * 2;
-  static constexpr size_t share_bytes = (size_t)kWaves * 2 * NHT * kWave * 16;
-  static constexpr size_t lds_bytes = park_bytes + 2 * share_bytes;
+  static constexpr int PC = RW / 8;                   // 16-byte pieces of a parked row
+  static constexpr int TL = CG == 4 ? 4 : 2;          // tiles of a group's step
+  static constexpr int STEP = TL * kTile;
+  static constexpr int U = TL / CG;                   // of them a wavefront's own: it makes their weights
+  // a wavefront's rows in LDS: the codes of a step and behind them the scales, in two places, or bf16 rows of two tiles
+  static constexpr int tile_bytes = NB * kTile * 16, place_bytes = TL * (tile_bytes + kWave * 4);
+  static constexpr int wave_bytes = 2 * place_bytes > 2 * kTile * RW * 2 ? 2 * place_bytes : 2 * kTile * RW * 2;
+  static constexpr size_t park_bytes = (size_t)kWaves * wave_bytes;
+  static constexpr size_t share_bytes = (size_t)SG * TL * (CG - 1) * kWave * 16;            // [group][tile][other wavefront][lane][4 slots]
+  static constexpr size_t weight_bytes = CG > 1 ? (size_t)SG * TL * kWave * 16 : 0;         // [group][pair of tiles][plane][lane][4 slots of either tile]
+  static constexpr size_t loop_bytes = park_bytes + 2 * share_bytes + 2 * weight_bytes;
+  static constexpr int OS = R + 4;                                                          // row stride of the groups' sums when they are merged (floats)
+  static constexpr size_t merge_bytes = SG > 1 ? (size_t)SG * 16 * OS * 4 : 0;
+  static constexpr size_t body_bytes = loop_bytes > merge_bytes ? loop_bytes : merge_bytes;
+  static constexpr size_t top_bytes = (size_t)kWaves * 16 * 4;                              // [wavefront][head]
+  static constexpr size_t lds_bytes = body_bytes + 2 * top_bytes + 2 * kWaves * 4;          // and whether a wavefront's weights need another reference
 };
 
-// What a lane has to do with a tile: constant for the kernel.
+// Where a wavefront's and a lane's part of everything is: constant for the kernel.
 template <class C>
 struct LaneMap {
-  int l16, g, wv;
-  int col;                 // its first latent column
-  int rope;                // its first RoPE column (of a lane that has none: a readable one)
-  bool has_lat, has_rope;
-  __device__ __forceinline__ LaneMap(int lane, int wv_) : l16(lane & 15), g(lane >> 4), wv(wv_) {
-    has_lat = !C::kMixed || g < 2;
-    col = wv * C::RW + (C::kMixed ? 8 * (g & 1) : C::LN * g);
-    const int rg = C::kMixed ? g - 2 : g;
-    has_rope = rg >= 0 && 8 * rg < C::DRW;
-    rope = wv * C::DRW + (has_rope ? 8 * rg : 0);
+  int lane, l16, g, wv, cg, sg;
+  int col;                      // the lane's first latent column (of a lane that has none: another's)
+  int rope[C::KR];              // its first RoPE column in a K step (likewise)
+  bool has_lat, has_rope[C::KR];
+  // a step's tile that is this wavefront's h-th: its own U first, and h = 0, 1 and h = 2, 3 a pair of neighbours
+  __device__ __forceinline__ int tile(int h) const { return C::CG == 1 ? h : (C::U * cg) ^ h; }
+  __device__ __forceinline__ int pair(int k) const { return tile(2 * k) >> 1; }
+  __device__ __forceinline__ LaneMap(int lane_, int wv_) : lane(lane_), l16(lane_ & 15), g(lane_ >> 4), wv(wv_), cg(wv_ % C::CG), sg(wv_ / C::CG) {
+    has_lat = g < C::NB;
+    col = cg * C::RW + kPackBlock * (g % C::NB);
+#pragma unroll
+    for (int t = 0; t < C::KR; ++t) {
+      const int c = 32 * t + 8 * g;
+      has_rope[t] = c < C::DRW;
+      rope[t] = cg * C::DRW + (has_rope[t] ? c : 0);
+    }
   }
 };
 
-// The table entries of 64 pages from `at` on, one a lane, clamped into the pool that they belong to.
-struct Pages64 {
+// The table entries of 64 pages, one a lane, clamped into the pool that they belong to.  A lookup is a
+// v_readlane: as a load it would be one more in flight in front of the tile's own, and every wait for a tile one for all of them.
+struct ChunkPages {
   int at, entry;
 };
 
 template <class C>
 struct PackedTile {  // as loaded
-  uint32_t code[C::CW];
-  uint32_t scale;
-  u32x4_t xr;
+  u32x4_t code;
+  uint32_t scale;    // of four slots (a byte would be widened where the registers go round, a wait for a load just issued)
+  u32x4_t xr[C::KR];
 };
 template <class C>
 struct OpenTile {
-  u32x4_t xc[C::CW];
-  u32x4_t xr;
+  u32x4_t xc[4];     // 32 latents
+  u32x4_t xr[C::KR];
 };
-
 struct Source {  // of one sequence
   const uint8_t* codes;
   const uint8_t* scales;
@@ -89,306 +124,704 @@ struct Source {  // of one sequence
   int n_packed, n_pages, n_pages4, shift, last_entry;
 };
 
-__device__ __forceinline__ void fetch_pages(Pages64& p, const Source& s, int at, int lane) {
+// (Both tables are read: which one counts need not be known yet.)
+struct PageEntries {
+  int packed, open;
+  __device__ __forceinline__ void load(const Source& s, int at, int lane) {
+    const int k = at + lane < s.last_entry ? at + lane : s.last_entry;
+    packed = s.table4[k];
+    open = s.table[k];
+  }
+};
+__device__ __forceinline__ ChunkPages chunk_pages(const PageEntries& e, const Source& s, int at, int lane) {
   const int k = at + lane < s.last_entry ? at + lane : s.last_entry;
   const bool packed = k < s.n_packed;
-  p.at = at;
-  p.entry = clamp_page(packed ? s.table4[k] : s.table[k], packed ? s.n_pages4 : s.n_pages);
+  return ChunkPages{at, clamp_page(packed ? e.packed : e.open, packed ? s.n_pages4 : s.n_pages)};
 }
 // Tile of the pool (in units of 16 slots) that holds slot s0 (wavefront-uniform, a multiple of 16).
-__device__ __forceinline__ uint32_t pool_tile(Pages64& p, const Source& s, int s0, int lane) {
-  const int k = s0 >> s.shift;
-  if (k - p.at >= kWave) fetch_pages(p, s, k, lane);
-  const int e = __builtin_amdgcn_readlane(p.entry, k - p.at);
+__device__ __forceinline__ uint32_t pool_tile(const ChunkPages& p, const Source& s, int s0) {
+  const int e = __builtin_amdgcn_readlane(p.entry, (s0 >> s.shift) - p.at);
   return ((uint32_t)e << (s.shift - 4)) + (uint32_t)((s0 & ((1 << s.shift) - 1)) >> 4);
 }
 
 template <class C>
 __device__ __forceinline__ void load_tile(PackedTile<C>& t, const Source& s, uint32_t tile, const LaneMap<C>& m) {
-  const uint8_t* c = s.codes + (size_t)tile * packed_code_bytes(C::R);
   const uint32_t unit = (uint32_t)(m.col / kPackBlock) * kTile + m.l16;
-  const uint8_t* from = c + unit * 16 + (m.col % kPackBlock) / 2;
-  if constexpr (C::CW == 4) {
-    const u32x4_t v = *reinterpret_cast<const u32x4_t*>(from);
-    t.code[0] = v[0], t.code[1] = v[1], t.code[2] = v[2], t.code[3] = v[3];
-  } else if constexpr (C::CW == 2) {
-    const uint2 v = *reinterpret_cast<const uint2*>(from);
-    t.code[0] = v.x, t.code[1] = v.y;
-  } else {
-    t.code[0] = *reinterpret_cast<const uint32_t*>(from);
-  }
-  t.scale = s.scales[(size_t)tile * packed_scale_bytes(C::R) + unit];
-  t.xr = *reinterpret_cast<const u32x4_t*>(s.keys + (size_t)tile * (packed_key_bytes(C::DR) / 2) + ((uint32_t)(m.rope / 8) * kTile + m.l16) * 8);
+  t.code = *reinterpret_cast<const u32x4_t*>(s.codes + (size_t)tile * packed_code_bytes(C::R) + unit * 16);
+  t.scale = *reinterpret_cast<const uint32_t*>(s.scales + (size_t)tile * packed_scale_bytes(C::R) + (unit & ~3u));
+#pragma unroll
+  for (int k = 0; k < C::KR; ++k)
+    t.xr[k] = *reinterpret_cast<const u32x4_t*>(s.keys + (size_t)tile * (packed_key_bytes(C::DR) / 2) + ((uint32_t)(m.rope[k] / 8) * kTile + m.l16) * 8);
 }
 template <class C>
 __device__ __forceinline__ void load_tile(OpenTile<C>& t, const Source& s, uint32_t tile, const LaneMap<C>& m) {
   const size_t row = (size_t)tile * kTile + m.l16;
-  const uint16_t* c = s.lat + row * C::R + m.col;
 #pragma unroll
-  for (int i = 0; i < C::CW; ++i) t.xc[i] = *reinterpret_cast<const u32x4_t*>(c + 8 * i);
-  t.xr = *reinterpret_cast<const u32x4_t*>(s.key + row * C::DR + m.rope);
+  for (int i = 0; i < 4; ++i) t.xc[i] = *reinterpret_cast<const u32x4_t*>(s.lat + row * C::R + m.col + 8 * i);
+#pragma unroll
+  for (int k = 0; k < C::KR; ++k) t.xr[k] = *reinterpret_cast<const u32x4_t*>(s.key + row * C::DR + m.rope[k]);
 }
 
+// Slots that are none of the sequence's count as zeros, whatever their bytes are.  `live`: of the tile's slots.
 template <class C>
-struct Operand {  // a lane's latents, 8 a piece, and its RoPE columns as bf16
-  u32x4_t lat[C::CW], rope;
-  __device__ __forceinline__ u32x4_t step(int kk, const LaneMap<C>& m) const {
-    if constexpr (C::kMixed) {
-      u32x4_t v;
+__device__ __forceinline__ void drop(PackedTile<C>& t, int live, const LaneMap<C>& m) {
+  if (m.l16 >= live) {
+    t.code = u32x4_t{0, 0, 0, 0};
+    t.scale = 0x7f7f7f7fu;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) v[i] = m.has_lat ? lat[0][i] : rope[i];
-      return v;
+    for (int k = 0; k < C::KR; ++k) t.xr[k] = u32x4_t{0, 0, 0, 0};
+  }
+}
+template <class C>
+__device__ __forceinline__ void drop(OpenTile<C>& t, int live, const LaneMap<C>& m) {
+  if (m.l16 >= live) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) t.xc[i] = u32x4_t{0, 0, 0, 0};
+#pragma unroll
+    for (int k = 0; k < C::KR; ++k) t.xr[k] = u32x4_t{0, 0, 0, 0};
+  }
+}
+
+// Heads past the last one are copies of it and never stored.
+template <class C>
+__device__ __forceinline__ const uint16_t* query_row(const uint16_t* rows, int n_heads, const LaneMap<C>& m) {
+  return rows + (size_t)(m.l16 < n_heads ? m.l16 : n_heads - 1) * C::E;
+}
+// The RoPE columns: two bf16 planes; a lane without a column holds zeros.
+template <class C>
+struct QueryRope {
+  u32x4_t hi[C::KR], lo[C::KR];
+  __device__ __forceinline__ void load(const uint16_t* rows, size_t plane, int n_heads, const LaneMap<C>& m) {
+#pragma unroll
+    for (int k = 0; k < C::KR; ++k) {
+      const uint16_t* from = query_row<C>(rows, n_heads, m) + C::R + m.rope[k];
+      const uint32_t mask = m.has_rope[k] ? 0xffffffffu : 0u;
+      hi[k] = *reinterpret_cast<const u32x4_t*>(from) & mask;
+      lo[k] = *reinterpret_cast<const u32x4_t*>(from + plane) & mask;
+    }
+  }
+};
+// The latent columns, for bf16 rows: the planes as they are.
+template <class C>
+struct QueryRows {
+  u32x4_t hi[4], lo[4];
+  __device__ __forceinline__ void load(const uint16_t* rows, size_t plane, int n_heads, const LaneMap<C>& m) {
+    const uint32_t mask = m.has_lat ? 0xffffffffu : 0u;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint16_t* from = query_row<C>(rows, n_heads, m) + m.col + 8 * i;
+      hi[i] = *reinterpret_cast<const u32x4_t*>(from) & mask;
+      lo[i] = *reinterpret_cast<const u32x4_t*>(from + plane) & mask;
+    }
+  }
+};
+// The latent columns, for codes: a lane's 32 numbers (a head's block) as four planes of E2M3 numbers (steps of 1/8 below 2, 1/4 below 4, 1/2 up to 7.5).  With
+// s the smallest power of two of which the largest is at most 7.5 times: the first plane is off by s / 4 at most; the second, in units of s / 16, sees
+// numbers up to 4 and is off by 1/8 of its unit, s / 128; so on in units of s / 512 and s / 2^14: s 2^-17, the largest number times 2^-18.9, at the end.
+template <class C>
+struct QueryPlanes {
+  u32x6_t plane[4];
+  uint32_t scale;  // the planes' exponents, a byte each
+  __device__ __forceinline__ void make(const QueryRows<C>& q) {
+    f32x16_t even, odd;
+    float top = 0.f, nan = 0.f;  // (fmaxf drops a NaN; it and an infinity make the block's logits NaN)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const u32x4_t hi = q.hi[i], lo = q.lo[i];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const float x = __uint_as_float(hi[j] << 16) + __uint_as_float(lo[j] << 16), y = __uint_as_float(hi[j] & 0xffff0000u) + __uint_as_float(lo[j] & 0xffff0000u);
+        top = fmaxf(top, fmaxf(fabsf(x), fabsf(y)));
+        nan = fmaf(0.f, x, fmaf(0.f, y, nan));
+        even[4 * i + j] = x;
+        odd[4 * i + j] = y;
+      }
+    }
+    const uint32_t tb = __float_as_uint(top);
+    int e = (int)(tb >> 23) - 2 + ((tb & 0x7fffffu) > 0x700000u ? 1 : 0);
+    e = nan == 0.f ? (e < 16 ? 16 : e) : 255;
+    constexpr int kDown[4] = {0, 4, 9, 14};
+    scale = 0;
+#pragma unroll
+    for (int p = 0; p < 4; ++p) {
+      const uint32_t ep = (uint32_t)(e == 255 ? 255 : e - kDown[p]);
+      scale |= ep << (8 * p);
+      const float unit = __uint_as_float(ep << 23);
+      // packed number 2i is the first operand's i-th, 2i + 1 the second's
+      u32x6_t code = __builtin_amdgcn_cvt_scalef32_2xpk16_fp6_f32(even, odd, unit);
+      asm volatile("" : "+v"(code) : "v"(even), "v"(odd), "v"(unit));  // (else the compiler lets the result overlap the operands, which the instruction reads to its end)
+      plane[p] = code;
+      if (p < 3) {
+        f32x32_t back = __builtin_amdgcn_cvt_scalef32_pk32_f32_fp6(code, unit);
+        asm volatile("" : "+v"(back) : "v"(code), "v"(unit));
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          even[i] -= back[2 * i];
+          odd[i] -= back[2 * i + 1];
+        }
+      }
+    }
+  }
+};
+
+// The state of one wavefront and what it does with it.
+template <class C>
+struct Worker {
+  static constexpr int MT = C::MT, CG = C::CG, U = C::U, TL = C::TL;
+  const LaneMap<C>& m;
+  unsigned char* smem;
+  int k1;                       // end of the slots that are attended here
+  float m_ref;                  // head l16's softmax reference, the same in all wavefronts of the group
+  float l_run;                  // normaliser, of the lane's slots of this wavefront's weights only
+  float4_t o[MT];               // sums over this wavefront's columns
+  float4_t sh[TL];              // this wavefront's share of a step's logits
+  float4_t sv[U], pw[U];        // its own tiles' logits (log2 units: the query is pre-scaled) and weights
+  bf16x8_t ph, pl;              // two tiles' weights as operands
+
+  __device__ __forceinline__ Worker(const LaneMap<C>& m_, unsigned char* smem_) : m(m_), smem(smem_), k1(0), m_ref(-INFINITY), l_run(0.f) {
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) o[mt] = float4_t{0.f, 0.f, 0.f, 0.f};
+  }
+  __device__ __forceinline__ float4_t* shares(int par) const {
+    return reinterpret_cast<float4_t*>(smem + C::park_bytes + par * C::share_bytes) + m.sg * (TL * (CG - 1) * kWave) + m.lane;
+  }
+  __device__ __forceinline__ u32x4_t* weights(int par) const {
+    return reinterpret_cast<u32x4_t*>(smem + C::park_bytes + 2 * C::share_bytes + par * C::weight_bytes) + m.sg * TL * kWave + m.lane;
+  }
+  __device__ __forceinline__ float* tops() const { return reinterpret_cast<float*>(smem + C::body_bytes); }
+  __device__ __forceinline__ int* flags(int par) const { return reinterpret_cast<int*>(smem + C::body_bytes + 2 * C::top_bytes) + par * kWaves; }
+
+  __device__ __forceinline__ void barrier() const {  // of the wavefronts that share slots
+    if constexpr (CG > 1) __syncthreads();
+  }
+
+  // ---- logits of a step: rows in a lane's registers against the query
+  __device__ __forceinline__ void rope_logits(const u32x4_t (&xr)[C::KR], const QueryRope<C>& q, int h) {
+#pragma unroll
+    for (int k = 0; k < C::KR; ++k) {
+      const bf16x8_t x = __builtin_bit_cast(bf16x8_t, xr[k]);
+      sh[h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, __builtin_bit_cast(bf16x8_t, q.hi[k]), sh[h], 0, 0, 0);
+      sh[h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, __builtin_bit_cast(bf16x8_t, q.lo[k]), sh[h], 0, 0, 0);
+    }
+  }
+  __device__ __forceinline__ void logits(const PackedTile<C> (&t)[TL], const QueryPlanes<C>& q, const QueryRope<C>& qr) {
+#pragma unroll
+    for (int h = 0; h < TL; ++h) {
+      const i32x8_t a = {(int)t[h].code[0], (int)t[h].code[1], (int)t[h].code[2], (int)t[h].code[3], 0, 0, 0, 0};
+      const int sa = (int)(t[h].scale >> (8 * (m.l16 & 3)));  // (the lowest byte counts)
+      auto plane = [&](auto p_, float4_t c) __attribute__((always_inline)) {
+        constexpr int p = decltype(p_)::value;
+        const u32x6_t b = q.plane[p];
+        const i32x8_t bv = {(int)b[0], (int)b[1], (int)b[2], (int)b[3], (int)b[4], (int)b[5], 0, 0};
+        return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, bv, c, /*A: E2M1*/ 4, /*B: E2M3*/ 2, 0, sa, p, (int)q.scale);
+      };
+      sh[h] = plane(std::integral_constant<int, 0>{}, float4_t{0.f, 0.f, 0.f, 0.f});
+      sh[h] = plane(std::integral_constant<int, 1>{}, sh[h]);
+      sh[h] = plane(std::integral_constant<int, 2>{}, sh[h]);
+      sh[h] = plane(std::integral_constant<int, 3>{}, sh[h]);
+      rope_logits(t[h].xr, qr, h);
+    }
+  }
+  __device__ __forceinline__ void logits(const OpenTile<C> (&t)[TL], const QueryRows<C>& q, const QueryRope<C>& qr) {
+#pragma unroll
+    for (int h = 0; h < TL; ++h) {
+      sh[h] = float4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const bf16x8_t x = __builtin_bit_cast(bf16x8_t, t[h].xc[i]);
+        sh[h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, __builtin_bit_cast(bf16x8_t, q.hi[i]), sh[h], 0, 0, 0);
+        sh[h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, __builtin_bit_cast(bf16x8_t, q.lo[i]), sh[h], 0, 0, 0);
+      }
+      rope_logits(t[h].xr, qr, h);
+    }
+  }
+  template <class Tile>
+  __device__ __forceinline__ void drop_dead(Tile (&t)[TL], int base) const {
+    if (base + C::STEP > k1) {  // (uniform; the last step's at most)
+#pragma unroll
+      for (int h = 0; h < TL; ++h) drop<C>(t[h], k1 - base - m.tile(h) * kTile, m);
+    }
+  }
+
+  // ---- the group's shares meet
+  __device__ __forceinline__ void put_shares(int par) const {
+    float4_t* to = shares(par);
+#pragma unroll
+    for (int h = U; h < TL; ++h) to[(m.tile(h) * (CG - 1) + h / U - 1) * kWave] = sh[h];
+  }
+  // this wavefront's own tiles (its share of them is still in `sh`)
+  __device__ __forceinline__ void get_logits(int par) {
+    const float4_t* from = shares(par);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      sv[u] = sh[u];
+#pragma unroll
+      for (int w = 0; w < CG - 1; ++w) sv[u] += from[(m.tile(u) * (CG - 1) + w) * kWave];
+    }
+  }
+  __device__ __forceinline__ int any_flag(int par) const {
+    if constexpr (CG == 1) return 0;
+    const int4 f = *reinterpret_cast<const int4*>(flags(par));
+    return f.x | f.y | f.z | f.w;
+  }
+
+  // ---- weights of a step, relative to a reference that is fixed at the first live step and moved only where a step tops it by more than 2^kRebase
+  __device__ __forceinline__ float top() const {
+    float t = fmaxf(fmaxf(sv[0][0], sv[0][1]), fmaxf(sv[0][2], sv[0][3]));
+    if constexpr (U == 2) t = fmaxf(t, fmaxf(fmaxf(sv[1][0], sv[1][1]), fmaxf(sv[1][2], sv[1][3])));
+    return t;
+  }
+  __device__ __forceinline__ void put_weights(int par) {
+    const float ref = m_ref == -INFINITY ? 0.f : m_ref;
+    u32x4_t h = {}, l = {};
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      uint32_t hi[2], lo[2];
+#pragma unroll
+      for (int v = 0; v < 4; ++v) pw[u][v] = __builtin_amdgcn_exp2f(sv[u][v] - ref);
+      split_bf16x2(pw[u][0], pw[u][1], hi[0], lo[0]);
+      split_bf16x2(pw[u][2], pw[u][3], hi[1], lo[1]);
+      if constexpr (CG == 1) {
+        h[2 * u] = hi[0], h[2 * u + 1] = hi[1];
+        l[2 * u] = lo[0], l[2 * u + 1] = lo[1];
+      } else {
+        const int t = m.tile(u);
+        uint2* to = reinterpret_cast<uint2*>(weights(par) + (t >> 1) * (2 * kWave)) + (t & 1);
+        to[0] = make_uint2(hi[0], hi[1]);
+        to[2 * kWave] = make_uint2(lo[0], lo[1]);
+      }
+    }
+    if constexpr (CG == 1) {
+      ph = __builtin_bit_cast(bf16x8_t, h);
+      pl = __builtin_bit_cast(bf16x8_t, l);
+    }
+  }
+  __device__ __forceinline__ void add_weights() {
+#pragma unroll
+    for (int u = 0; u < U; ++u) l_run += (pw[u][0] + pw[u][1]) + (pw[u][2] + pw[u][3]);
+  }
+  __device__ __forceinline__ void move_ref(float to) {
+    const float alpha = m_ref == to ? 1.f : __builtin_amdgcn_exp2f(m_ref - to);
+    m_ref = to;
+    l_run *= alpha;
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) o[mt] *= alpha;
+  }
+  // Logits `sv` of the step at `base` -> weights, in the place `par`.  CG = 1: the reference moves at once (everything formed with the old one is in `o`);
+  // else a wavefront that sees that it has to says so, and settle() forms the group's weights again, behind a barrier.
+  __device__ __forceinline__ void make_weights(int par, int base) {
+    if (base + C::STEP > k1) {
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int v = 0; v < 4; ++v)
+          if (base + m.tile(u) * kTile + 4 * m.g + v >= k1) sv[u][v] = -INFINITY;
+    }
+    const float t = top();
+    const bool moves = m_ref == -INFINITY ? t > -INFINITY : t - m_ref > kRebase;
+    if constexpr (CG == 1) {
+      if (__any(moves)) move_ref(fmaxf(m_ref, quarter_reduce(t, LaneMax())));
     } else {
-      return kk < C::KC ? lat[kk < C::KC ? kk : 0] : rope;
+      flags(par)[m.wv] = __any(moves) ? 1 : 0;
+    }
+    put_weights(par);
+  }
+  // Behind the barrier after make_weights(par), with any_flag(par): true weights in their place.  All wavefronts of the workgroup take the same way.
+  __device__ __forceinline__ void settle(int par, int flag) {
+    if constexpr (CG > 1) {
+      if (__builtin_amdgcn_readfirstlane(flag)) {
+        const float t = quarter_reduce(top(), LaneMax());
+        if (m.g == 0) tops()[m.wv * 16 + m.l16] = t;
+        __syncthreads();
+        float to = m_ref;
+#pragma unroll
+        for (int w = 0; w < CG; ++w) to = fmaxf(to, tops()[(m.sg * CG + w) * 16 + m.l16]);
+        move_ref(to);
+        put_weights(par);
+        __syncthreads();
+      }
+    }
+    add_weights();
+  }
+  __device__ __forceinline__ void get_weights(int par, int pair) {
+    if constexpr (CG > 1) {
+      ph = __builtin_bit_cast(bf16x8_t, weights(par)[pair * 2 * kWave]);
+      pl = __builtin_bit_cast(bf16x8_t, weights(par)[pair * 2 * kWave + kWave]);
     }
   }
-};
 
-// live: whether the lane's slot is one of the sequence's; a dead one counts as zeros whatever its bytes are
-template <class C>
-__device__ __forceinline__ void to_operand(Operand<C>& x, const PackedTile<C>& t, bool live) {
-  const float scale = __uint_as_float((live ? t.scale : 127u) << 23);
+  // ---- values of codes.  A tile's codes lie in LDS as in memory, [block][slot][16 bytes].  A transposing read of bytes gives lane (l16, g) byte l16, that is
+  // columns 2 l16 and 2 l16 + 1 of a block, of the eight slots whose weights it holds; they become bf16 pairs (v_cvt_scalef32_pk_bf16_fp4, exact; of the scale
+  // operand only the exponent counts, so a shift brings a slot's byte there), and two slots' pairs one dword of either column's operand.
+  // Column of o[2 nb + par][i] of lane (l16, g): 32 nb + 8 g + 2 i + par.
+  __device__ __forceinline__ unsigned char* codes_at(int par) const { return smem + m.wv * C::wave_bytes + par * C::place_bytes; }
+  __device__ __forceinline__ void park(const PackedTile<C> (&t)[TL], int par) const {
+    unsigned char* to = codes_at(par);
 #pragma unroll
-  for (int i = 0; i < C::CW; ++i) {
-    const uint32_t c = live ? t.code[i] : 0u;
-    x.lat[i][0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, scale, 0));
-    x.lat[i][1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, scale, 1));
-    x.lat[i][2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, scale, 2));
-    x.lat[i][3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, scale, 3));
-  }
-#pragma unroll
-  for (int i = 0; i < 4; ++i) x.rope[i] = live ? t.xr[i] : 0u;
-}
-template <class C>
-__device__ __forceinline__ void to_operand(Operand<C>& x, const OpenTile<C>& t, bool live) {
-#pragma unroll
-  for (int i = 0; i < C::CW; ++i)
-#pragma unroll
-    for (int j = 0; j < 4; ++j) x.lat[i][j] = live ? t.xc[i][j] : 0u;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) x.rope[i] = live ? t.xr[i] : 0u;
-}
-
-template <class C>
-struct Query {
-  u32x4_t hi[C::NHT][C::KQ], lo[C::NHT][C::KQ];
-};
-// Heads past the last one are copies of it and never stored; lanes without a column of a step hold zeros, whatever their rows hold.
-template <class C>
-__device__ __forceinline__ void load_query(Query<C>& q, const uint16_t* rows, size_t plane, int n_heads, const LaneMap<C>& m) {
-#pragma unroll
-  for (int ht = 0; ht < C::NHT; ++ht) {
-    const int h = 16 * ht + m.l16 < n_heads ? 16 * ht + m.l16 : n_heads - 1;
-    const uint16_t* row = rows + (size_t)h * C::E;
-#pragma unroll
-    for (int kk = 0; kk < C::KQ; ++kk) {
-      const bool rope_step = kk == C::KC;
-      const uint16_t* from = rope_step ? (C::kMixed && m.has_lat ? row + m.col : row + C::R + m.rope) : row + m.col + 8 * kk;
-      const uint32_t mask = !rope_step || m.has_rope || (C::kMixed && m.has_lat) ? 0xffffffffu : 0u;
-      q.hi[ht][kk] = *reinterpret_cast<const u32x4_t*>(from) & mask;
-      q.lo[ht][kk] = *reinterpret_cast<const u32x4_t*>(from + plane) & mask;
+    for (int h = 0; h < TL; ++h) {
+      if (m.has_lat) *reinterpret_cast<u32x4_t*>(to + m.tile(h) * C::tile_bytes + m.lane * 16) = t[h].code;
+      // [tile][block][slot], exponents of floats
+      reinterpret_cast<uint32_t*>(to + TL * C::tile_bytes)[m.tile(h) * kWave + m.lane] = (t[h].scale >> (8 * (m.l16 & 3))) << 23;
     }
   }
-}
-
-template <class C>
-struct Sums {  // m_ref: the same in all wavefronts; l_run: this lane's slots only; o: this wavefront's columns
-  float m_ref[C::NHT], l_run[C::NHT];
-  float4_t o[C::NHT][C::MT];
-  __device__ __forceinline__ void reset() {
-#pragma unroll
-    for (int ht = 0; ht < C::NHT; ++ht) {
-      m_ref[ht] = -INFINITY;
-      l_run[ht] = 0.f;
-#pragma unroll
-      for (int mt = 0; mt < C::MT; ++mt) o[ht][mt] = float4_t{0.f, 0.f, 0.f, 0.f};
-    }
-  }
-};
-
-// Slots [k0, k1) of one kind of page, k0 a multiple of 16 and k0 < k1.
-template <class C, class Tile, int NS>
-__device__ __forceinline__ void stream(const Source& s, Pages64& pages, const Query<C>& q, Sums<C>& ws, unsigned char* smem, int k0, int k1, int& par,
-                                       const LaneMap<C>& m, int lane) {
-  uint16_t* park = reinterpret_cast<uint16_t*>(smem) + m.wv * kStep * C::TS;
-  const int last = (k1 - 1) & ~(kTile - 1);  // the last tile with a live slot: beyond it, copies of it are loaded and count as dead
-  Tile t[NS][2];
-  auto load = [&](Tile (&to)[2], int base) __attribute__((always_inline)) {
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const int s0 = base + h * kTile < last ? base + h * kTile : last;
-      load_tile<C>(to[h], s, pool_tile(pages, s, __builtin_amdgcn_readfirstlane(s0), lane), m);
-    }
+  struct CodeRows {  // of two tiles
+    i32x2_t code[C::NB];
+    u32x4_t scale[C::NB][2];
   };
+  __device__ __forceinline__ void get_codes(CodeRows& x, int par, int pair) const {
+    const unsigned char* from = codes_at(par);
+    const int row = m.l16 >> 1;
+    const unsigned char* at = from + (2 * pair + (row >> 2)) * C::tile_bytes + (4 * m.g + (row & 3)) * 16 + 8 * (m.l16 & 1);
 #pragma unroll
-  for (int st = 0; st < NS; ++st) load(t[st], k0 + st * kStep);
-  for (int base = k0; base < k1;) {
+    for (int nb = 0; nb < C::NB; ++nb) x.code[nb] = __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_int2_ptr)(const int*)(at + nb * (kTile * 16)));
 #pragma unroll
-    for (int st = 0; st < NS; ++st) {
-      if (base >= k1) break;
-      float4_t* shares = reinterpret_cast<float4_t*>(smem + C::park_bytes + (size_t)par * C::share_bytes);
-      // ---- this wavefront's share of the logits (log2 units: the query is pre-scaled), and its slice of the latents for the value product
+    for (int nb = 0; nb < C::NB; ++nb)
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+        x.scale[nb][h] = *reinterpret_cast<const u32x4_t*>(from + TL * C::tile_bytes + ((2 * pair + h) * kWave + nb * kTile + 4 * m.g) * 4);
+  }
+  __device__ __forceinline__ void add_codes(const CodeRows& x) {
+#pragma unroll
+    for (int nb = 0; nb < C::NB; ++nb) {
+      u32x4_t even, odd;
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        Operand<C> x;
-        to_operand<C>(x, t[st][h], base + h * kTile + m.l16 < k1);
-#pragma unroll
-        for (int ht = 0; ht < C::NHT; ++ht) {
-          float4_t s0 = float4_t{0.f, 0.f, 0.f, 0.f}, s1 = s0;
-#pragma unroll
-          for (int kk = 0; kk < C::KQ; ++kk) {
-            const bf16x8_t xv = __builtin_bit_cast(bf16x8_t, x.step(kk, m));
-            s0 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(xv, __builtin_bit_cast(bf16x8_t, q.hi[ht][kk]), s0, 0, 0, 0);
-            s1 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(xv, __builtin_bit_cast(bf16x8_t, q.lo[ht][kk]), s1, 0, 0, 0);
-          }
-          shares[((m.wv * 2 + h) * C::NHT + ht) * kWave + lane] = s0 + s1;
-        }
-        if (m.has_lat) {
-          uint16_t* to = park + (h * kTile + m.l16) * C::TS + (m.col - m.wv * C::RW);
-#pragma unroll
-          for (int i = 0; i < C::CW; ++i) *reinterpret_cast<u32x4_t*>(to + 8 * i) = x.lat[i];
-        }
+        const uint32_t c = (uint32_t)x.code[nb][h];
+        const u32x4_t e = x.scale[nb][h];
+        const uint32_t s0 = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, __uint_as_float(e[0]), 0));
+        const uint32_t s1 = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, __uint_as_float(e[1]), 1));
+        const uint32_t s2 = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, __uint_as_float(e[2]), 2));
+        const uint32_t s3 = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, __uint_as_float(e[3]), 3));
+        even[2 * h] = __builtin_amdgcn_perm(s1, s0, 0x05040100u);
+        odd[2 * h] = __builtin_amdgcn_perm(s1, s0, 0x07060302u);
+        even[2 * h + 1] = __builtin_amdgcn_perm(s3, s2, 0x05040100u);
+        odd[2 * h + 1] = __builtin_amdgcn_perm(s3, s2, 0x07060302u);
       }
-      load(t[st], base + NS * kStep);
-      __syncthreads();  // all shares are in LDS
-      // ---- weights: lane holds head l16 of a head tile and slots 4g .. 4g + 3 of both tiles
-      bf16x8_t ph[C::NHT], pl[C::NHT];
+      add_value(2 * nb, __builtin_bit_cast(bf16x8_t, even));
+      add_value(2 * nb + 1, __builtin_bit_cast(bf16x8_t, odd));
+    }
+  }
+  __device__ __forceinline__ void add_value(int mt, bf16x8_t x) {
+    o[mt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, ph, o[mt], 0, 0, 0);
+    o[mt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, pl, o[mt], 0, 0, 0);
+  }
+
+  // ---- values of bf16 rows, through the wavefront's own LDS too: a block's even columns in front of its odd ones (the order of the sums).  Piece p of row i lies at
+  // place p ^ f(i): the 16 rows' writes of one piece go to all banks (f takes 16 values), and so do the transposing reads, 32 bytes of each of 8 rows.
+  __device__ __forceinline__ static int place(int row) { return (((row & 7) << 1) | ((row >> 3) & 1)) & (C::PC - 1); }
+  __device__ __forceinline__ void park_rows(const OpenTile<C> (&t)[TL], int k) const {
 #pragma unroll
-      for (int ht = 0; ht < C::NHT; ++ht) {
-        float sv[8];
+    for (int h = 2 * k; h < 2 * k + 2; ++h) park_row(t[h].xc, m.tile(h) & 1);
+  }
+  __device__ __forceinline__ void park_row(const u32x4_t (&x)[4], int h) const {
+    if (m.has_lat) {
+      unsigned char* to = smem + m.wv * C::wave_bytes + (h * kTile + m.l16) * (C::RW * 2);
+      const int p0 = (m.g % C::NB) * 4, f = place(m.l16);
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          float4_t sum = shares[(h * C::NHT + ht) * kWave + lane];
-#pragma unroll
-          for (int w = 1; w < kWaves; ++w) sum += shares[((w * 2 + h) * C::NHT + ht) * kWave + lane];
-#pragma unroll
-          for (int v = 0; v < 4; ++v) sv[4 * h + v] = base + h * kTile + 4 * m.g + v < k1 ? sum[v] : -INFINITY;
-        }
-        // relative to a reference that is fixed at the first live step and moved only where a step tops it by more than 2^kRebase
-        constexpr float kRebase = 40.f;
-        float top = fmaxf(fmaxf(fmaxf(sv[0], sv[1]), fmaxf(sv[2], sv[3])), fmaxf(fmaxf(sv[4], sv[5]), fmaxf(sv[6], sv[7])));
-        if (__any(ws.m_ref[ht] == -INFINITY || top - ws.m_ref[ht] > kRebase)) {
-          top = quarter_reduce(top, LaneMax());
-          if (ws.m_ref[ht] == -INFINITY) {
-            ws.m_ref[ht] = top;
-          } else if (top - ws.m_ref[ht] > kRebase) {
-            const float alpha = __builtin_amdgcn_exp2f(ws.m_ref[ht] - top);
-            ws.m_ref[ht] = top;
-            ws.l_run[ht] *= alpha;
-#pragma unroll
-            for (int mt = 0; mt < C::MT; ++mt) ws.o[ht][mt] *= alpha;
-          }
-        }
-        const float ref = ws.m_ref[ht] == -INFINITY ? 0.f : ws.m_ref[ht];
-        u32x4_t hi, lo;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const float p0 = __builtin_amdgcn_exp2f(sv[2 * j] - ref), p1 = __builtin_amdgcn_exp2f(sv[2 * j + 1] - ref);
-          uint32_t a, b;
-          split_bf16x2(p0, p1, a, b);
-          hi[j] = a;
-          lo[j] = b;
-          ws.l_run[ht] += p0 + p1;
-        }
-        ph[ht] = __builtin_bit_cast(bf16x8_t, hi);
-        pl[ht] = __builtin_bit_cast(bf16x8_t, lo);
+      for (int i = 0; i < 4; ++i) {
+        const u32x4_t &a = x[2 * (i & 1)], &b = x[2 * (i & 1) + 1];
+        const uint32_t sel = i < 2 ? 0x05040100u : 0x07060302u;
+        *reinterpret_cast<u32x4_t*>(to + 16 * ((p0 + i) ^ f)) = u32x4_t{__builtin_amdgcn_perm(a[1], a[0], sel), __builtin_amdgcn_perm(a[3], a[2], sel),
+                                                                       __builtin_amdgcn_perm(b[1], b[0], sel), __builtin_amdgcn_perm(b[3], b[2], sel)};
       }
-      // ---- O^T[col, head] += C_hat^T[col, slot] P^T[slot, head]: a transposing read hands a lane four slots of a column, two of them the operand
-      const uint16_t* trow = park + (4 * m.g + (m.l16 >> 2)) * C::TS + 4 * (m.l16 & 3);
+    }
+  }
+  __device__ __forceinline__ void add_rows() {
+    const int row = 4 * m.g + (m.l16 >> 2), f = place(row);
+    const unsigned char* at = smem + m.wv * C::wave_bytes + row * (C::RW * 2) + 8 * (m.l16 & 1);
+    const int piece = (m.l16 >> 1) & 1;  // of the two that a column tile has
 #pragma unroll
-      for (int mt = 0; mt < C::MT; ++mt) {
-        const short4_t c0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4_ptr)(trow + 16 * mt));
-        const short4_t c1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4_ptr)(trow + kTile * C::TS + 16 * mt));
-        typedef short short8_t __attribute__((ext_vector_type(8)));
-        const bf16x8_t cv = __builtin_bit_cast(bf16x8_t, (short8_t)__builtin_shufflevector(c0, c1, 0, 1, 2, 3, 4, 5, 6, 7));
+    for (int mt = 0; mt < MT; ++mt) {
+      const unsigned char* from = at + 16 * ((2 * mt + piece) ^ f);
+      const short4_t c0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4_ptr)(const short*)from);
+      const short4_t c1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4_ptr)(const short*)(from + kTile * C::RW * 2));
+      add_value(mt, __builtin_bit_cast(bf16x8_t, (short8_t)__builtin_shufflevector(c0, c1, 0, 1, 2, 3, 4, 5, 6, 7)));
+    }
+  }
+};
+
+// The tiles of a step of this wavefront's group, from slot `base` on; slots past `last` become copies of its tile.
+template <class C, int H0 = 0, int H1 = C::TL, class Tile>
+__device__ __forceinline__ void load_step(Tile (&t)[C::TL], const Source& s, ChunkPages& pages, int base, int last, const LaneMap<C>& m) {
+  constexpr int kAll = C::STEP * C::SG;
+  const int first = base - C::STEP * m.sg, to = ((first + kAll - 1 < last ? first + kAll - 1 : last) >> s.shift) - pages.at;
+  if (__builtin_amdgcn_readfirstlane(to) >= kWave) {  // (the next 64 pages)
+    pages.at = __builtin_amdgcn_readfirstlane((first < last ? first : last) >> s.shift);
+    PageEntries e;
+    e.load(s, pages.at, m.lane);
+    pages = chunk_pages(e, s, pages.at, m.lane);
+  }
 #pragma unroll
-        for (int ht = 0; ht < C::NHT; ++ht) {
-          ws.o[ht][mt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(cv, ph[ht], ws.o[ht][mt], 0, 0, 0);
-          ws.o[ht][mt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(cv, pl[ht], ws.o[ht][mt], 0, 0, 0);
-        }
-      }
-      par ^= 1;
-      base += kStep;
+  for (int h = H0; h < H1; ++h) {
+    const int s0 = base + m.tile(h) * kTile, s1 = s0 < last ? s0 : last;
+    load_tile<C>(t[h], s, pool_tile(pages, s, __builtin_amdgcn_readfirstlane(s1)), m);
+  }
+  __builtin_amdgcn_sched_barrier(0);  // in this order everywhere: the waits count the loads issued since
+}
+
+// Packed slots [k0, k1), k0 a multiple of 16, k0 < k1.  Between two barriers: values of step i - 1, weights of step i and logits of step i + 1 (of a step past the
+// last one: of copies, and nobody reads them).  The codes of step i + 1 take the place of those of step i - 1, behind their reads.
+template <class C, class Last>
+__device__ __forceinline__ void stream_packed(Worker<C>& w, const Source& s, ChunkPages& pages, const QueryPlanes<C>& q, const QueryRope<C>& qr, int k0,
+                                              int k1, Last&& before_last_values) {
+  const LaneMap<C>& m = w.m;
+  constexpr int kAll = C::STEP * C::SG;  // slots of a step of all groups
+  w.k1 = k1;
+  const int first = k0 + C::STEP * m.sg, last = (k1 - 1) & ~(kTile - 1), n = (k1 - k0 + kAll - 1) / kAll;
+  PackedTile<C> t[C::TL];
+  load_step<C>(t, s, pages, first, last, m);
+  auto logits = [&](int step) __attribute__((always_inline)) {
+    w.drop_dead(t, first + step * kAll);
+    w.logits(t, q, qr);
+    w.park(t, step & 1);
+    load_step<C>(t, s, pages, first + (step + 1) * kAll, last, m);
+  };
+  auto values = [&](int step) __attribute__((always_inline)) {
+    const int par = step & 1;
+    w.settle(par, w.any_flag(par));
+#pragma unroll
+    for (int pair = 0; pair < C::TL / 2; ++pair) {
+      typename Worker<C>::CodeRows x;
+      w.get_codes(x, par, pair);
+      w.get_weights(par, pair);
+      w.add_codes(x);
+    }
+  };
+  auto weights = [&](int step) __attribute__((always_inline)) {
+    w.get_logits(step & 1);
+    w.make_weights(step & 1, first + step * kAll);
+  };
+  auto meet = [&](int step) __attribute__((always_inline)) {
+    w.put_shares(step & 1);
+    w.barrier();
+  };
+  logits(0);
+  meet(0);
+  for (int i = 0; i < n; ++i) {
+    if (i > 0) values(i - 1);
+    weights(i);
+    logits(i + 1);
+    meet(i + 1);
+  }
+  before_last_values();
+  values(n - 1);
+}
+
+// Slots [k0, k1) of the bf16 pool, k0 a multiple of 16, k0 < k1: the few behind the packed ones, one step after the other.
+template <class C>
+struct OpenStep {
+  OpenTile<C> t[C::TL];
+  QueryRows<C> q;
+};
+template <class C, int H0, int H1>
+__device__ __forceinline__ void load_open(OpenStep<C>& o, const Source& s, ChunkPages& pages, int base, int k1, const LaneMap<C>& m) {
+  load_step<C, H0, H1>(o.t, s, pages, base + C::STEP * m.sg, (k1 - 1) & ~(kTile - 1), m);
+}
+template <class C>
+__device__ __forceinline__ void stream_open(Worker<C>& w, const Source& s, ChunkPages& pages, OpenStep<C>& o, const QueryRope<C>& qr, int k0, int k1) {
+  const LaneMap<C>& m = w.m;
+  constexpr int kAll = C::STEP * C::SG;
+  w.k1 = k1;
+  for (int at = k0; at < k1; at += kAll) {
+    const int base = at + C::STEP * m.sg;
+    const bool more = at + kAll < k1;
+    w.drop_dead(o.t, base);
+    w.logits(o.t, o.q, qr);
+    w.put_shares(0);
+    w.park_rows(o.t, 0);
+    if (more) load_open<C, 0, 2>(o, s, pages, at + kAll, k1, m);
+    w.barrier();
+    w.get_logits(0);
+    w.make_weights(0, base);
+    w.barrier();
+    w.settle(0, w.any_flag(0));
+    w.get_weights(0, m.pair(0));
+    w.add_rows();
+    if constexpr (C::TL > 2) {
+      w.park_rows(o.t, 1);
+      if (more) load_open<C, 2, C::TL>(o, s, pages, at + kAll, k1, m);
+      w.get_weights(0, m.pair(1));
+      w.add_rows();
     }
   }
 }
 
-// grid = (chunks, sequences, groups of up to 32 heads)
-template <int R, int DR, int NHT>
-__global__ __launch_bounds__(kBlock) void attn_packed_kernel(AttnPackedArgs a) {
-  using C = PackCfg<R, DR, NHT>;
-  extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
-  const int split = blockIdx.x, b = blockIdx.y, h0 = blockIdx.z * 32;
-  const int tid = threadIdx.x, lane = tid & (kWave - 1);
-  const int wv = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const LaneMap<C> m(lane, wv);
-  const AttnArgs& at = a.at;
-  const int heads = at.n_heads - h0 < 32 ? at.n_heads - h0 : 32;
+struct Run {  // slots [k0, k1) of sequence b, k0 < k1, k0 a multiple of 16
+  int b, k0, k1, piece;
+};
 
-  const int live = live_slots(load_uniform_i32(at.seq_len, b), at.stride, at.max_slots);
-  int n_packed = load_uniform_i32(a.pk.n_packed, b);
-  const int k0 = split * at.chunk, k1 = live < k0 + at.chunk ? live : k0 + at.chunk;
-  if (k0 >= k1) return;
-  n_packed = n_packed < 0 ? 0 : (n_packed < at.pages.max_pages ? n_packed : at.pages.max_pages);
+// What a run asks for ahead of everything that it has to know first.
+template <class C>
+struct RunHead {
+  PageEntries entries;
+  int n_packed;
+  QueryRope<C> qr;
+  QueryRows<C> q;
+};
+template <class C>
+__device__ __forceinline__ Source source_of(const AttnPackedArgs& a, int b) {
   Source s;
   s.codes = a.pk.codes;
   s.scales = a.pk.scales;
   s.keys = a.pk.keys;
-  s.lat = reinterpret_cast<const uint16_t*>(at.lat);
-  s.key = reinterpret_cast<const uint16_t*>(at.key);
-  s.table = at.pages.table + (size_t)b * at.pages.max_pages;
-  s.table4 = a.pk.table + (size_t)b * at.pages.max_pages;
-  s.n_packed = n_packed;
-  s.n_pages = at.pages.n_pages;
+  s.lat = reinterpret_cast<const uint16_t*>(a.at.lat);
+  s.key = reinterpret_cast<const uint16_t*>(a.at.key);
+  s.table = a.at.pages.table + (size_t)b * a.at.pages.max_pages;
+  s.table4 = a.pk.table + (size_t)b * a.at.pages.max_pages;
+  s.n_pages = a.at.pages.n_pages;
   s.n_pages4 = a.pk.n_pages;
-  s.shift = at.pages.shift;
-  s.last_entry = at.pages.max_pages - 1;
+  s.shift = a.at.pages.shift;
+  s.last_entry = a.at.pages.max_pages - 1;
+  return s;
+}
+template <class C>
+__device__ __forceinline__ const uint16_t* query_rows(const AttnArgs& at, int b, int h0) {
+  return reinterpret_cast<const uint16_t*>(at.qcat) + ((size_t)b * at.n_heads + h0) * C::E;
+}
+template <class C>
+__device__ __forceinline__ void load_head(RunHead<C>& h, const AttnPackedArgs& a, const Source& s, int b, int k0, const LaneMap<C>& m, int h0, int heads) {
+  h.n_packed = load_uniform_i32(a.pk.n_packed, b);
+  h.entries.load(s, k0 >> s.shift, m.lane);
+  h.q.load(query_rows<C>(a.at, b, h0), a.at.q_plane, heads, m);
+  h.qr.load(query_rows<C>(a.at, b, h0), a.at.q_plane, heads, m);
+}
 
-  Pages64 pages;
-  fetch_pages(pages, s, k0 >> s.shift, lane);
-  Query<C> q;
-  load_query<C>(q, reinterpret_cast<const uint16_t*>(at.qcat) + ((size_t)b * at.n_heads + h0) * C::E, at.q_plane, heads, m);
-  Sums<C> ws;
-  ws.reset();
+template <class C>
+__device__ __forceinline__ void attend_run(const AttnPackedArgs& a, const Run& run, RunHead<C>& head, Source& s, const LaneMap<C>& m, int h0, int heads, unsigned char* smem) {
+  constexpr int R = C::R;
+  const AttnArgs& at = a.at;
+  const int b = run.b, k0 = run.k0, k1 = run.k1, tid = threadIdx.x, wv = m.wv;
+  int n_packed = head.n_packed;
+  s.n_packed = n_packed = n_packed < 0 ? 0 : (n_packed < at.pages.max_pages ? n_packed : at.pages.max_pages);
+  const QueryRope<C>& qr = head.qr;
+  Worker<C> w(m, smem);
   const long long packed_slots = (long long)n_packed << s.shift;
   const int kp = (int)(packed_slots < k1 ? packed_slots : k1);  // slots below it come out of packed pages
-  int par = 0;
-  if (kp > k0) stream<C, PackedTile<C>, 2>(s, pages, q, ws, smem, k0, kp, par, m, lane);
   const int ko = kp > k0 ? kp : k0;
-  if (k1 > ko) stream<C, OpenTile<C>, 1>(s, pages, q, ws, smem, ko, k1, par, m, lane);
+  ChunkPages pages = chunk_pages(head.entries, s, k0 >> s.shift, m.lane);
+  OpenStep<C> o;
+  auto ask_for_open = [&]() __attribute__((always_inline)) {
+    if (k1 > ko) {
+      o.q.load(query_rows<C>(at, b, h0), at.q_plane, heads, m);
+      load_open<C, 0, C::TL>(o, s, pages, ko, k1, m);
+    }
+  };
+  if (kp > k0) {
+    QueryPlanes<C> q;
+    q.make(head.q);
+    stream_packed<C>(w, s, pages, q, qr, k0, kp, ask_for_open);
+  } else {
+    ask_for_open();
+  }
+  if (k1 > ko) stream_open<C>(w, s, pages, o, qr, ko, k1);
 
-  // ---- the chunk's partial: lane holds head l16, columns 16mt + 4g .. + 3
-  const size_t piece = (size_t)b * at.n_splits + split;
+  // ---- normalisers and references of the groups
+  float* part_l = w.tops();                              // [wavefront][head]
+  float* refs = part_l + kWaves * 16;                    // [group][head]
+  w.barrier();  // (the tops' place may have been in use)
+  const float l_wave = quarter_reduce(w.l_run, LaneSum());
+  if (m.g == 0) part_l[wv * 16 + m.l16] = l_wave;
+  if (m.g == 0 && m.cg == 0) refs[m.sg * 16 + m.l16] = w.m_ref;
+  const size_t piece = run.piece;
+  if constexpr (C::SG == 1) {
+    __syncthreads();
+    // ---- the chunk's partial: lane holds head l16, columns 32nb + 8g .. + 7
+    float l = 0.f;
 #pragma unroll
-  for (int ht = 0; ht < NHT; ++ht) {
-    const float l = quarter_reduce(ws.l_run[ht], LaneSum());
-    if (16 * ht + m.l16 < heads) {
-      const size_t oh = piece * at.n_heads + h0 + 16 * ht + m.l16;
-      const size_t col = oh * R + wv * C::RW + 4 * m.g;
+    for (int cg = 0; cg < C::CG; ++cg) l += part_l[cg * 16 + m.l16];
+    if (m.l16 < heads) {
+      const size_t oh = piece * at.n_heads + h0 + m.l16, col = oh * R + m.cg * C::RW + 8 * m.g;
       if (at.part_f16) {
         const float inv = 1.f / l;
         uint16_t* po = reinterpret_cast<uint16_t*>(at.part_o) + col;
 #pragma unroll
-        for (int mt = 0; mt < C::MT; ++mt)
-          *reinterpret_cast<uint2*>(po + 16 * mt) = make_uint2(pack_f16x2(ws.o[ht][mt][0] * inv, ws.o[ht][mt][1] * inv),
-                                                               pack_f16x2(ws.o[ht][mt][2] * inv, ws.o[ht][mt][3] * inv));
+        for (int nb = 0; nb < C::NB; ++nb) {
+          const float4_t a0 = w.o[2 * nb] * inv, a1 = w.o[2 * nb + 1] * inv;
+          *reinterpret_cast<uint4*>(po + 32 * nb) = make_uint4(pack_f16x2(a0[0], a1[0]), pack_f16x2(a0[1], a1[1]), pack_f16x2(a0[2], a1[2]), pack_f16x2(a0[3], a1[3]));
+        }
       } else {
 #pragma unroll
-        for (int mt = 0; mt < C::MT; ++mt) *reinterpret_cast<float4_t*>(at.part_o + col + 16 * mt) = ws.o[ht][mt];
+        for (int nb = 0; nb < C::NB; ++nb) {
+          const float4_t a0 = w.o[2 * nb], a1 = w.o[2 * nb + 1];
+          *reinterpret_cast<float4_t*>(at.part_o + col + 32 * nb) = float4_t{a0[0], a1[0], a0[1], a1[1]};
+          *reinterpret_cast<float4_t*>(at.part_o + col + 32 * nb + 4) = float4_t{a0[2], a1[2], a0[3], a1[3]};
+        }
       }
-      if (wv == 0 && m.g == 0) *reinterpret_cast<float2*>(at.part_ml + oh * 2) = make_float2(ws.m_ref[ht], l);
+      if (wv == 0 && m.g == 0) *reinterpret_cast<float2*>(at.part_ml + oh * 2) = make_float2(w.m_ref, l);
+    }
+  } else {
+    // ---- the groups' sums meet
+    float* sums = reinterpret_cast<float*>(smem);  // [group][head][OS]
+    __syncthreads();  // the parked rows' place
+    float* to = sums + (m.sg * 16 + m.l16) * C::OS + m.cg * C::RW + 8 * m.g;
+#pragma unroll
+    for (int nb = 0; nb < C::NB; ++nb) {
+      const float4_t a0 = w.o[2 * nb], a1 = w.o[2 * nb + 1];
+      *reinterpret_cast<float4_t*>(to + 32 * nb) = float4_t{a0[0], a1[0], a0[1], a1[1]};
+      *reinterpret_cast<float4_t*>(to + 32 * nb + 4) = float4_t{a0[2], a1[2], a0[3], a1[3]};
+    }
+    __syncthreads();
+    constexpr int R4 = R / 4;
+    for (int i = tid; i < heads * R4; i += kBlock) {
+      const int h = i / R4, c4 = i - h * R4;
+      float ref[C::SG], top = -INFINITY, l = 0.f;
+#pragma unroll
+      for (int sg = 0; sg < C::SG; ++sg) {
+        ref[sg] = refs[sg * 16 + h];
+        top = fmaxf(top, ref[sg]);
+      }
+      float4_t sum = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int sg = 0; sg < C::SG; ++sg) {
+        const float f = __builtin_amdgcn_exp2f(ref[sg] - top);  // 0 for a group that saw no slot
+        sum += f * *reinterpret_cast<const float4_t*>(sums + (sg * 16 + h) * C::OS + 4 * c4);
+#pragma unroll
+        for (int cg = 0; cg < C::CG; ++cg) l += f * part_l[(sg * C::CG + cg) * 16 + h];
+      }
+      const size_t oh = piece * at.n_heads + h0 + h, col = oh * R + 4 * c4;
+      if (at.part_f16) {
+        const float inv = 1.f / l;
+        *reinterpret_cast<uint2*>(reinterpret_cast<uint16_t*>(at.part_o) + col) = make_uint2(pack_f16x2(sum[0] * inv, sum[1] * inv), pack_f16x2(sum[2] * inv, sum[3] * inv));
+      } else {
+        *reinterpret_cast<float4_t*>(at.part_o + col) = sum;
+      }
+      if (c4 == 0) *reinterpret_cast<float2*>(at.part_ml + oh * 2) = make_float2(top, l);
     }
   }
 }
 
-template <int R, int DR, int NHT>
+// grid = (sequences, tiles of 16 heads, chunks): the head tiles of a chunk run side by side and find its bytes in the caches (32 heads in one workgroup need
+// twice the registers, and few long sequences have too few workgroups); sequences side by side go to different XCDs.
+template <int R, int DR>
+__global__ __launch_bounds__(kBlock, 2) void attn_packed_kernel(AttnPackedArgs a) {
+  using C = PackCfg<R, DR>;
+  extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
+  const int tid = threadIdx.x, lane = tid & (kWave - 1), h0 = blockIdx.y * 16;
+  const int wv = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const LaneMap<C> m(lane, wv);
+  const AttnArgs& at = a.at;
+  const int heads = at.n_heads - h0 < 16 ? at.n_heads - h0 : 16;
+  Run run;
+  run.b = blockIdx.x;
+  run.k0 = blockIdx.z * at.chunk;
+  const int len = load_uniform_i32(at.seq_len, run.b);
+  Source s = source_of<C>(a, run.b);
+  RunHead<C> head;
+  load_head<C>(head, a, s, run.b, run.k0, m, h0, heads);
+  const int live = live_slots(len, at.stride, at.max_slots);
+  run.k1 = live - run.k0 < at.chunk ? live : run.k0 + at.chunk;
+  run.piece = run.b * at.n_splits + blockIdx.z;
+  if (run.k0 < run.k1) attend_run<C>(a, run, head, s, m, h0, heads, smem);
+}
+
+template <int R, int DR>
 hipError_t launch_one(const AttnPackedArgs& a, hipStream_t st, const EventPair& ev) {
-  using C = PackCfg<R, DR, NHT>;
+  using C = PackCfg<R, DR>;
   static DeviceSet lds_allowed;
-  const hipError_t e = allow_lds(&attn_packed_kernel<R, DR, NHT>, C::lds_bytes, lds_allowed);
+  const hipError_t e = allow_lds(&attn_packed_kernel<R, DR>, C::lds_bytes, lds_allowed);
   if (e != hipSuccess) return e;
-  const dim3 grid(a.at.n_splits, a.at.batch, (a.at.n_heads + 31) / 32);
-  launch_timed(attn_packed_kernel<R, DR, NHT>, grid, dim3(kBlock), C::lds_bytes, st, ev, a);
+  const dim3 grid(a.at.batch, (a.at.n_heads + 15) / 16, a.at.n_splits);
+  launch_timed(attn_packed_kernel<R, DR>, grid, dim3(kBlock), C::lds_bytes, st, ev, a);
   return hipGetLastError();
 }
 
@@ -397,7 +830,7 @@ hipError_t launch_one(const AttnPackedArgs& a, hipStream_t st, const EventPair& 
 hipError_t launch_attn_packed(const AttnPackedArgs& a, hipStream_t st, const EventPair& ev) {
 #define MTLA_CASE(RR, DD)                       \
   if (a.at.r == RR && a.at.d_rope == DD)        \
-    return a.at.n_heads <= 16 ? launch_one<RR, DD, 1>(a, st, ev) : launch_one<RR, DD, 2>(a, st, ev);
+    return launch_one<RR, DD>(a, st, ev);
   MTLA_CASE(64, 32)
   MTLA_CASE(64, 64)
   MTLA_CASE(128, 32)

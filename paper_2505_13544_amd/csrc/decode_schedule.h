@@ -11,6 +11,16 @@ constexpr int decode_chunk(int max_batch, int max_slots) {
   return (int)(chunk < 64 ? 64 : (chunk > 1024 ? 1024 : chunk));
 }
 
+// The same over packed pages, whose kernel gives every 16 heads workgroups of their own; and no more than 256 chunks of a sequence, which one workgroup a head
+// joins.  us of attention + join at r = 512, chunks of 128 / 256 / 512 / 1024 slots:
+//   8 x 8192, 32 heads     24.8 + 8.9 / 19.6 + 7.0 / 21.4 + 6.3 / 31.3 + 6.5
+//   1 x 131071, 16 heads   26.6 + 38.1 / 22.2 + 21.4 / 27.5 + 13.4 / 38.0 + 9.5
+//   256 x 256 to 2048, 16 heads   82.0 + 14.1 / 65.4 + 11.1 / 57.0 + 9.3 / 51.8 + 8.7
+constexpr int packed_chunk(int max_batch, int max_slots, int n_heads) {
+  const int even = decode_chunk(max_batch * ((n_heads + 15) / 16), max_slots), least = (max_slots / 256 + 64) / 64 * 64;
+  return even > least ? even : least;
+}
+
 // Whether a call of `batch` sequences of up to `max_slots` slots takes the balanced schedule rather than static chunks; `chunk_set`: by the caller.
 // The balanced one has a fixed cost, the scan of the lengths and a cold start of every persistent workgroup, some 5 us of a step beside a
 // chunk a workgroup, and its partials are halves.  Below 8 tiles of 16 slots a unit it is left out: with partials in fp32, as the chunks' are, it would gain there only with

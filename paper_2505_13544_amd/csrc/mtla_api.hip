@@ -48,12 +48,21 @@ constexpr int kMaxPersistent = 1024;
 constexpr int kRunCost = 6;
 constexpr int kBalancedMaxBatch = 2048;  // the running tile counts of a batch live in LDS
 
+// Slots of a chunk over packed pages, and their number.
+inline int packed_chunk(const mtla_ctx* c) { return c->chunk_set ? c->chunk : mtla::packed_chunk(c->cfg.max_batch, c->cfg.max_slots, c->cfg.n_heads); }
+inline int packed_splits(const mtla_ctx* c) { return (c->cfg.max_slots + packed_chunk(c) - 1) / packed_chunk(c); }
+
 // Partials ("pieces") the decode pass can emit: chunks x sequences under the static schedule,
 // one per persistent workgroup plus one per sequence under the balanced one.
 inline size_t max_pieces(const mtla_ctx* c) {
+  size_t most = (size_t)kMaxPersistent + c->cfg.max_batch;
   const size_t stat = (size_t)c->cfg.max_batch * n_splits(c);
-  const size_t bal = (size_t)kMaxPersistent + c->cfg.max_batch;
-  return stat > bal ? stat : bal;
+  if (stat > most) most = stat;
+  if (c->cfg.page_slots > 0) {
+    const size_t packed = (size_t)c->cfg.max_batch * packed_splits(c);
+    if (packed > most) most = packed;
+  }
+  return most;
 }
 
 // Decode workspace:
@@ -708,6 +717,7 @@ static mtla_status decode_packed_core(mtla_ctx* c, const AppendArgs* ap, const v
       (w_uv && !aligned16(w_uv)))
     return MTLA_ERR_INVALID_ARG;
   if (c->prefix_owner) return MTLA_ERR_UNSUPPORTED;  // with pages a shared prompt is shared pages
+  if (packed_splits(c) > 65535) return MTLA_ERR_UNSUPPORTED;  // a grid dimension: a very small chunk of very long sequences
   hipStream_t st = reinterpret_cast<hipStream_t>(hip_stream);
   char* ws = reinterpret_cast<char*>(workspace);
   const DecodeLayout L = decode_layout(c);
@@ -741,8 +751,8 @@ static mtla_status decode_packed_core(mtla_ctx* c, const AppendArgs* ap, const v
   cb.d_head = g.d_head;
   cb.stride = g.stride;
   cb.max_slots = g.max_slots;
-  cb.chunk = c->chunk;
-  cb.n_splits = n_splits(c);
+  cb.chunk = packed_chunk(c);
+  cb.n_splits = packed_splits(c);
   cb.batch = batch;
   cb.T = 0;
   cb.n_persistent = 0;
