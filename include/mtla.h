@@ -451,7 +451,8 @@ typedef struct {
  *   slot_map   device int64 [batch, n_new_max] or NULL: the row of the pool (page * page_slots + slot in it) that
  *              token t of sequence b goes to; -1 for padding, beyond the capacity, and for a refused sequence's
  *              tokens without a page
- *   workspace  device, the context's workspace (status word)
+ *   workspace  device, the context's workspace: the status word and, for more than 64 sequences, sums in the place
+ *              of a step's query, so not beside a decode call with the same workspace on another stream
  */
 mtla_status mtla_pages_fit(mtla_ctx* ctx, const mtla_page_pool* pool, const mtla_page_pool* packed /*nullable*/,
                            const int32_t* seq_len, const int32_t* n_new, int32_t n_new_max, int32_t keep_pages,

@@ -692,6 +692,7 @@ mtla_status mtla_pages_fit(mtla_ctx* c, const mtla_page_pool* pool, const mtla_p
   a.n_new = n_new;
   a.slot_map = slot_map;
   a.status = reinterpret_cast<int32_t*>(workspace);
+  a.scratch = reinterpret_cast<char*>(workspace) + decode_layout(c).qcat;  // (a step's query: every step writes it before it reads it)
   a.n_new_max = n_new_max;
   a.keep_pages = keep_pages;
   a.batch = batch;

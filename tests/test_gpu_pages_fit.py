@@ -181,3 +181,51 @@ def test_words_that_hold_anything_stay_inside_the_arrays():
             inside[at:at + size] = True
         assert bool((arena[~inside] == -5).all()), word
         assert 0 <= int(t["state"][0]) < pages and 0 <= int(t["state"][1]) <= pages
+
+
+@pytest.mark.parametrize("batch", [64, 65, 80, 1024, 1025])
+def test_many_sequences_and_too_few_pages(batch):
+    # either pool short of pages, then both, then room for all again: who gets pages depends on who came before, across every group of sequences
+    rng = np.random.default_rng(batch)
+    t = Tables(max_batch=batch, max_slots=128, page_slots=16, stride=1, n_pages=batch * 5, n_packed=batch * 2, spill=True)
+    lens, some = np.zeros(batch, np.int64), 0
+    for step in range(6):
+        n = rng.integers(0, 60, batch)
+        some += t.fit(lens, n, 60, what=f"step {step}")
+        lens = np.minimum(lens + n, 128)
+        lens[rng.random(batch) < 0.3] = 0
+        t.fit(lens, None, 1, what=f"behind step {step}")
+    assert some > 0
+    assert t.fit(np.zeros(batch, np.int64), what="all leave") == 0
+    assert t.fit(np.zeros(batch, np.int64), np.full(batch, 30), 30, what="and come back") == 0
+
+
+def test_words_that_hold_anything_among_many_sequences():
+    # as above, with the sequences dealt to several workgroups and two pools
+    n, mp, pages = 300, 4, 900
+    ctx = B.Context(n_heads=4, d_head=64, r=64, d_rope=32, d_hyper=64, stride=1, max_batch=n, max_slots=64, dtype="bf16", page_slots=16, n_pages=pages)
+    ws = torch.zeros(ctx.workspace_bytes(), dtype=torch.uint8, device=DEV)
+    rng = np.random.default_rng(1)
+    sizes = dict(table=(n, mp), first=(n,), end=(n,), ring=(pages,), state=(4,), was_end=(n,))
+    for word in (-(1 << 31), -1, 3, 100, (1 << 31) - 1):
+        arena = torch.full((16384,), -5, dtype=torch.int32, device=DEV)
+        inside = torch.zeros(16384, dtype=torch.bool, device=DEV)
+        at, pools = 64, []
+        for _ in range(2):
+            t = {}
+            for k, shape in sizes.items():
+                size = int(np.prod(shape))
+                t[k] = arena[at:at + size].view(*shape)
+                t[k].copy_(dev(rng.integers(0, mp, shape).astype(np.int32)))
+                inside[at:at + size] = True
+                at += size + 64
+            t["state"][0], t["state"][1] = word, word
+            for k in ("first", "end"):
+                t[k][int(rng.integers(n))] = word
+            pools.append(t)
+        ctx.pages_fit(B.PagePool(**pools[0]), B.PagePool(**pools[1]), dev(rng.integers(-3, 70, n).astype(np.int32)), None, 4, 0, n, None, ws,
+                      torch.cuda.current_stream().cuda_stream)
+        ctx.device_status(ws, torch.cuda.current_stream().cuda_stream)
+        assert bool((arena[~inside] == -5).all()), word
+        for t in pools:
+            assert 0 <= int(t["state"][0]) < pages and 0 <= int(t["state"][1]) <= pages
