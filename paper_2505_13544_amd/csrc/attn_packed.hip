@@ -16,11 +16,11 @@
 // rounding to bf16 (one plane would add as much again).  The normaliser sums the unrounded weights.
 //
 // Between two barriers a wavefront forms the values of step i - 1, the weights of step i and the logits of step i + 1.  What bounds it, r = 512, 16 heads:
-//   512 x 1024 slots (two workgroups a unit)  53 us, 4.0 TB/s: half the time VALU, a quarter MFMA, and the memory (47 us with all pages in L2)
-//   256 x 1024 slots (one)                    32 us, 3.3 TB/s: what a step waits for, one after the other (0.7 us for 32 slots)
-//   256 x 32 slots                            10 us: the launch and three reads that wait for each other
+//   512 x 1024 slots (two workgroups a unit)  52 us, 4.0 TB/s: half the time VALU, a quarter MFMA, and the memory (47 us with all pages in L2)
+//   256 x 1024 slots, chunks of 512           33 us, 3.2 TB/s: a step of 64 slots is 1.7 us alone on a unit, 2.4 beside another workgroup's
+//   256 x 32 slots                            9 us: the launch, two reads that wait for each other (0.7 us each, 1.6 with all units reading), an open step (2.3)
 // An equal share of all steps for each of 512 workgroups took 47 us instead of 49 where 256 lengths range from 256 to 2048 slots, and 37 instead of 32 where all are
-// 1024: its scan of the lengths is one more read to wait for.
+// 1024: its scan of the lengths is one more read to wait for.  The open page in front of the packed ones, or its rows asked for ahead of the last step's values: no gain.
 #include "bounds.h"
 #include "lds_stream.h"
 #include "mtla_device.h"
@@ -276,7 +276,10 @@ struct Worker {
   float4_t o[MT];               // sums over this wavefront's columns
   float4_t sh[TL];              // this wavefront's share of a step's logits
   float4_t sv[U], pw[U];        // its own tiles' logits (log2 units: the query is pre-scaled) and weights
-  bf16x8_t ph, pl;              // two tiles' weights as operands
+  struct Weights {              // two tiles' weights as operands
+    bf16x8_t hi, lo;
+  };
+  Weights own;                  // CG = 1: those of the step
 
   __device__ __forceinline__ Worker(const LaneMap<C>& m_, unsigned char* smem_) : m(m_), smem(smem_), k1(0), m_ref(-INFINITY), l_run(0.f) {
 #pragma unroll
@@ -322,10 +325,11 @@ struct Worker {
       rope_logits(t[h].xr, qr, h);
     }
   }
-  __device__ __forceinline__ void logits(const OpenTile<C> (&t)[TL], const QueryRows<C>& q, const QueryRope<C>& qr) {
+  __device__ __forceinline__ void logits(const OpenTile<C> (&t)[TL], const QueryRows<C>& q, const QueryRope<C>& qr, int base) {
 #pragma unroll
     for (int h = 0; h < TL; ++h) {
       sh[h] = float4_t{0.f, 0.f, 0.f, 0.f};
+      if (base + m.tile(h) * kTile >= k1) continue;  // (uniform: a page of a sequence is half empty)
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const bf16x8_t x = __builtin_bit_cast(bf16x8_t, t[h].xc[i]);
@@ -350,13 +354,13 @@ struct Worker {
     for (int h = U; h < TL; ++h) to[(m.tile(h) * (CG - 1) + h / U - 1) * kWave] = sh[h];
   }
   // this wavefront's own tiles (its share of them is still in `sh`)
-  __device__ __forceinline__ void get_logits(int par) {
+  __device__ __forceinline__ void get_logits(int par, float4_t (&to)[U]) const {
     const float4_t* from = shares(par);
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      sv[u] = sh[u];
+      to[u] = sh[u];
 #pragma unroll
-      for (int w = 0; w < CG - 1; ++w) sv[u] += from[(m.tile(u) * (CG - 1) + w) * kWave];
+      for (int w = 0; w < CG - 1; ++w) to[u] += from[(m.tile(u) * (CG - 1) + w) * kWave];
     }
   }
   __device__ __forceinline__ int any_flag(int par) const {
@@ -392,8 +396,8 @@ struct Worker {
       }
     }
     if constexpr (CG == 1) {
-      ph = __builtin_bit_cast(bf16x8_t, h);
-      pl = __builtin_bit_cast(bf16x8_t, l);
+      own.hi = __builtin_bit_cast(bf16x8_t, h);
+      own.lo = __builtin_bit_cast(bf16x8_t, l);
     }
   }
   __device__ __forceinline__ void add_weights() {
@@ -427,7 +431,7 @@ struct Worker {
     put_weights(par);
   }
   // Behind the barrier after make_weights(par), with any_flag(par): true weights in their place.  All wavefronts of the workgroup take the same way.
-  __device__ __forceinline__ void settle(int par, int flag) {
+  __device__ __forceinline__ bool settle(int par, int flag) {  // whether they changed
     if constexpr (CG > 1) {
       if (__builtin_amdgcn_readfirstlane(flag)) {
         const float t = quarter_reduce(top(), LaneMax());
@@ -439,15 +443,16 @@ struct Worker {
         move_ref(to);
         put_weights(par);
         __syncthreads();
+        add_weights();
+        return true;
       }
     }
     add_weights();
+    return false;
   }
-  __device__ __forceinline__ void get_weights(int par, int pair) {
-    if constexpr (CG > 1) {
-      ph = __builtin_bit_cast(bf16x8_t, weights(par)[pair * 2 * kWave]);
-      pl = __builtin_bit_cast(bf16x8_t, weights(par)[pair * 2 * kWave + kWave]);
-    }
+  __device__ __forceinline__ Weights get_weights(int par, int pair) const {
+    if constexpr (CG == 1) return own;
+    return Weights{__builtin_bit_cast(bf16x8_t, weights(par)[pair * 2 * kWave]), __builtin_bit_cast(bf16x8_t, weights(par)[pair * 2 * kWave + kWave])};
   }
 
   // ---- values of codes.  A tile's codes lie in LDS as in memory, [block][slot][16 bytes].  A transposing read of bytes gives lane (l16, g) byte l16, that is
@@ -464,46 +469,43 @@ struct Worker {
       reinterpret_cast<uint32_t*>(to + TL * C::tile_bytes)[m.tile(h) * kWave + m.lane] = (t[h].scale >> (8 * (m.l16 & 3))) << 23;
     }
   }
-  struct CodeRows {  // of two tiles
-    i32x2_t code[C::NB];
-    u32x4_t scale[C::NB][2];
+  struct CodeRows {  // of a block of two tiles
+    i32x2_t code;
+    u32x4_t scale[2];
   };
-  __device__ __forceinline__ void get_codes(CodeRows& x, int par, int pair) const {
+  __device__ __forceinline__ void get_codes(CodeRows& x, int par, int pair, int nb) const {
     const unsigned char* from = codes_at(par);
     const int row = m.l16 >> 1;
     const unsigned char* at = from + (2 * pair + (row >> 2)) * C::tile_bytes + (4 * m.g + (row & 3)) * 16 + 8 * (m.l16 & 1);
+    x.code = __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_int2_ptr)(const int*)(at + nb * (kTile * 16)));
 #pragma unroll
-    for (int nb = 0; nb < C::NB; ++nb) x.code[nb] = __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_int2_ptr)(const int*)(at + nb * (kTile * 16)));
-#pragma unroll
-    for (int nb = 0; nb < C::NB; ++nb)
-#pragma unroll
-      for (int h = 0; h < 2; ++h)
-        x.scale[nb][h] = *reinterpret_cast<const u32x4_t*>(from + TL * C::tile_bytes + ((2 * pair + h) * kWave + nb * kTile + 4 * m.g) * 4);
+    for (int h = 0; h < 2; ++h)
+      x.scale[h] = *reinterpret_cast<const u32x4_t*>(from + TL * C::tile_bytes + ((2 * pair + h) * kWave + nb * kTile + 4 * m.g) * 4);
   }
-  __device__ __forceinline__ void add_codes(const CodeRows& x) {
+  __device__ __forceinline__ void add_codes(const CodeRows& x, const Weights& p, int nb) {
+    u32x4_t even, odd;
 #pragma unroll
-    for (int nb = 0; nb < C::NB; ++nb) {
-      u32x4_t even, odd;
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const uint32_t c = (uint32_t)x.code[nb][h];
-        const u32x4_t e = x.scale[nb][h];
-        const uint32_t s0 = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, __uint_as_float(e[0]), 0));
-        const uint32_t s1 = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, __uint_as_float(e[1]), 1));
-        const uint32_t s2 = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, __uint_as_float(e[2]), 2));
-        const uint32_t s3 = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, __uint_as_float(e[3]), 3));
-        even[2 * h] = __builtin_amdgcn_perm(s1, s0, 0x05040100u);
-        odd[2 * h] = __builtin_amdgcn_perm(s1, s0, 0x07060302u);
-        even[2 * h + 1] = __builtin_amdgcn_perm(s3, s2, 0x05040100u);
-        odd[2 * h + 1] = __builtin_amdgcn_perm(s3, s2, 0x07060302u);
-      }
-      add_value(2 * nb, __builtin_bit_cast(bf16x8_t, even));
-      add_value(2 * nb + 1, __builtin_bit_cast(bf16x8_t, odd));
+    for (int h = 0; h < 2; ++h) {
+      const uint32_t c = (uint32_t)x.code[h];
+      const u32x4_t e = x.scale[h];
+      const uint32_t s0 = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, __uint_as_float(e[0]), 0));
+      const uint32_t s1 = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, __uint_as_float(e[1]), 1));
+      const uint32_t s2 = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, __uint_as_float(e[2]), 2));
+      const uint32_t s3 = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, __uint_as_float(e[3]), 3));
+      even[2 * h] = __builtin_amdgcn_perm(s1, s0, 0x05040100u);
+      odd[2 * h] = __builtin_amdgcn_perm(s1, s0, 0x07060302u);
+      even[2 * h + 1] = __builtin_amdgcn_perm(s3, s2, 0x05040100u);
+      odd[2 * h + 1] = __builtin_amdgcn_perm(s3, s2, 0x07060302u);
     }
+    const bf16x8_t a = __builtin_bit_cast(bf16x8_t, even), b = __builtin_bit_cast(bf16x8_t, odd);
+    o[2 * nb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, p.hi, o[2 * nb], 0, 0, 0);
+    o[2 * nb + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b, p.hi, o[2 * nb + 1], 0, 0, 0);
+    o[2 * nb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, p.lo, o[2 * nb], 0, 0, 0);
+    o[2 * nb + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b, p.lo, o[2 * nb + 1], 0, 0, 0);
   }
   __device__ __forceinline__ void add_value(int mt, bf16x8_t x) {
-    o[mt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, ph, o[mt], 0, 0, 0);
-    o[mt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, pl, o[mt], 0, 0, 0);
+    o[mt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, own.hi, o[mt], 0, 0, 0);
+    o[mt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, own.lo, o[mt], 0, 0, 0);
   }
 
   // ---- values of bf16 rows, through the wavefront's own LDS too: a block's even columns in front of its odd ones (the order of the sums).  Piece p of row i lies at
@@ -561,34 +563,47 @@ __device__ __forceinline__ void load_step(Tile (&t)[C::TL], const Source& s, Chu
 
 // Packed slots [k0, k1), k0 a multiple of 16, k0 < k1.  Between two barriers: values of step i - 1, weights of step i and logits of step i + 1 (of a step past the
 // last one: of copies, and nobody reads them).  The codes of step i + 1 take the place of those of step i - 1, behind their reads.
-template <class C, class Last>
-__device__ __forceinline__ void stream_packed(Worker<C>& w, const Source& s, ChunkPages& pages, const QueryPlanes<C>& q, const QueryRope<C>& qr, int k0,
-                                              int k1, Last&& before_last_values) {
+template <class C>
+__device__ __forceinline__ void stream_packed(Worker<C>& w, const Source& s, ChunkPages& pages, const QueryRows<C>& rows, const QueryRope<C>& qr, int k0,
+                                              int k1) {
   const LaneMap<C>& m = w.m;
   constexpr int kAll = C::STEP * C::SG;  // slots of a step of all groups
   w.k1 = k1;
   const int first = k0 + C::STEP * m.sg, last = (k1 - 1) & ~(kTile - 1), n = (k1 - k0 + kAll - 1) / kAll;
   PackedTile<C> t[C::TL];
   load_step<C>(t, s, pages, first, last, m);
+  QueryPlanes<C> q;
+  q.make(rows);  // (1.6 us: the first step's bytes come in meanwhile)
   auto logits = [&](int step) __attribute__((always_inline)) {
     w.drop_dead(t, first + step * kAll);
     w.logits(t, q, qr);
     w.park(t, step & 1);
     load_step<C>(t, s, pages, first + (step + 1) * kAll, last, m);
   };
+  // A block (of two tiles) after the other, the reads of the next two under way: left to itself the compiler puts every read in front of its use, ten waits a step.
   auto values = [&](int step) __attribute__((always_inline)) {
-    const int par = step & 1;
-    w.settle(par, w.any_flag(par));
+    constexpr int NB = C::NB, kBlocks = NB * C::TL / 2, kAhead = 2;
+    const int par = step & 1, flag = w.any_flag(par);
+    typename Worker<C>::Weights p = w.get_weights(par, 0), p_next = p;
+    typename Worker<C>::CodeRows x[kAhead + 1];
 #pragma unroll
-    for (int pair = 0; pair < C::TL / 2; ++pair) {
-      typename Worker<C>::CodeRows x;
-      w.get_codes(x, par, pair);
-      w.get_weights(par, pair);
-      w.add_codes(x);
+    for (int j = 0; j < kAhead; ++j) w.get_codes(x[j], par, j / NB, j % NB);
+    __builtin_amdgcn_sched_barrier(0);
+    if (w.settle(par, flag)) p = w.get_weights(par, 0);
+#pragma unroll
+    for (int j = 0; j < kBlocks; ++j) {
+      const int next = j + kAhead;
+      if (next < kBlocks) {
+        w.get_codes(x[next % (kAhead + 1)], par, next / NB, next % NB);
+        if (next % NB == 0) p_next = w.get_weights(par, next / NB);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+      if (j > 0 && j % NB == 0) p = p_next;
+      w.add_codes(x[j % (kAhead + 1)], p, j % NB);
     }
   };
   auto weights = [&](int step) __attribute__((always_inline)) {
-    w.get_logits(step & 1);
+    w.get_logits(step & 1, w.sv);
     w.make_weights(step & 1, first + step * kAll);
   };
   auto meet = [&](int step) __attribute__((always_inline)) {
@@ -603,7 +618,6 @@ __device__ __forceinline__ void stream_packed(Worker<C>& w, const Source& s, Chu
     logits(i + 1);
     meet(i + 1);
   }
-  before_last_values();
   values(n - 1);
 }
 
@@ -626,22 +640,27 @@ __device__ __forceinline__ void stream_open(Worker<C>& w, const Source& s, Chunk
     const int base = at + C::STEP * m.sg;
     const bool more = at + kAll < k1;
     w.drop_dead(o.t, base);
-    w.logits(o.t, o.q, qr);
+    w.logits(o.t, o.q, qr, base);
     w.put_shares(0);
-    w.park_rows(o.t, 0);
+    const auto live = [&](int k) { return base + 2 * m.pair(k) * kTile < k1; };
+    if (live(0)) w.park_rows(o.t, 0);
     if (more) load_open<C, 0, 2>(o, s, pages, at + kAll, k1, m);
     w.barrier();
-    w.get_logits(0);
+    w.get_logits(0, w.sv);
     w.make_weights(0, base);
     w.barrier();
     w.settle(0, w.any_flag(0));
-    w.get_weights(0, m.pair(0));
-    w.add_rows();
-    if constexpr (C::TL > 2) {
-      w.park_rows(o.t, 1);
-      if (more) load_open<C, 2, C::TL>(o, s, pages, at + kAll, k1, m);
-      w.get_weights(0, m.pair(1));
+    if (live(0)) {
+      w.own = w.get_weights(0, m.pair(0));
       w.add_rows();
+    }
+    if constexpr (C::TL > 2) {
+      if (live(1)) w.park_rows(o.t, 1);
+      if (more) load_open<C, 2, C::TL>(o, s, pages, at + kAll, k1, m);
+      if (live(1)) {
+        w.own = w.get_weights(0, m.pair(1));
+        w.add_rows();
+      }
     }
   }
 }
@@ -690,7 +709,7 @@ template <class C>
 __device__ __forceinline__ void attend_run(const AttnPackedArgs& a, const Run& run, RunHead<C>& head, Source& s, const LaneMap<C>& m, int h0, int heads, unsigned char* smem) {
   constexpr int R = C::R;
   const AttnArgs& at = a.at;
-  const int b = run.b, k0 = run.k0, k1 = run.k1, tid = threadIdx.x, wv = m.wv;
+  const int k0 = run.k0, k1 = run.k1, tid = threadIdx.x, wv = m.wv;
   int n_packed = head.n_packed;
   s.n_packed = n_packed = n_packed < 0 ? 0 : (n_packed < at.pages.max_pages ? n_packed : at.pages.max_pages);
   const QueryRope<C>& qr = head.qr;
@@ -699,21 +718,13 @@ __device__ __forceinline__ void attend_run(const AttnPackedArgs& a, const Run& r
   const int kp = (int)(packed_slots < k1 ? packed_slots : k1);  // slots below it come out of packed pages
   const int ko = kp > k0 ? kp : k0;
   ChunkPages pages = chunk_pages(head.entries, s, k0 >> s.shift, m.lane);
-  OpenStep<C> o;
-  auto ask_for_open = [&]() __attribute__((always_inline)) {
-    if (k1 > ko) {
-      o.q.load(query_rows<C>(at, b, h0), at.q_plane, heads, m);
-      load_open<C, 0, C::TL>(o, s, pages, ko, k1, m);
-    }
-  };
-  if (kp > k0) {
-    QueryPlanes<C> q;
-    q.make(head.q);
-    stream_packed<C>(w, s, pages, q, qr, k0, kp, ask_for_open);
-  } else {
-    ask_for_open();
+  if (kp > k0) stream_packed<C>(w, s, pages, head.q, qr, k0, kp);
+  if (k1 > ko) {
+    OpenStep<C> o;
+    o.q.load(query_rows<C>(at, run.b, h0), at.q_plane, heads, m);
+    load_open<C, 0, C::TL>(o, s, pages, ko, k1, m);
+    stream_open<C>(w, s, pages, o, qr, ko, k1);
   }
-  if (k1 > ko) stream_open<C>(w, s, pages, o, qr, ko, k1);
 
   // ---- normalisers and references of the groups
   float* part_l = w.tops();                              // [wavefront][head]
