@@ -507,8 +507,12 @@ mtla_status mtla_pages_unpack(mtla_ctx* ctx, void* cache_c, void* cache_kr, cons
  * sees to that).  Arguments, checks and errors as there, any n_heads and d_head, but
  *   out   device elem [batch, n_heads, d_head] or NULL: bf16, what W_O's product takes; its rounding is the largest
  *         error behind the packing (sums, weights and normalisers are fp32 or better than 16 bits)
- * mtla_set_decode_chunk applies; mtla_set_decode_schedule does not.  Not together with mtla_set_shared_prefix
- * (MTLA_ERR_UNSUPPORTED).
+ * A head's absorbed query enters the products with the codes as numbers that are off by at most 2^-18 of the largest
+ * of their 32 latents' (2^-17 of themselves over bf16 pages): what a query asks of a latent 2^18 times less than of
+ * its neighbour is not heard.
+ * mtla_set_decode_chunk applies (0: a rule of this call's own, from the context's sequences and heads);
+ * mtla_set_decode_schedule does not.  MTLA_ERR_UNSUPPORTED: more than 65535 chunks of max_slots (a small chunk that
+ * the caller set), or together with mtla_set_shared_prefix.
  */
 mtla_status mtla_decode_attn_packed(mtla_ctx* ctx, const void* q, const void* q_rope, const void* w_uk, const void* w_uv,
                                     const void* cache_c, const void* cache_kr, const int32_t* seq_len,

@@ -200,6 +200,7 @@ class Case:
                 assert not o[b].any() and not ol[b].any() and np.all(np.isneginf(ls[b])), where
                 continue
             # logits: q~ as two bf16 numbers (off by 2^-17 of itself, 2^-16 allows for its own sum), sums of r + d_R terms in fp32
+            # (over packed pages off by 2^-18.9 of the largest of 32, three to four times the mean of normal numbers: 2^-17 of itself on average)
             de = bd["logit"] * (2.0 ** -16 + (self.r + self.d_rope + self.d_head) * 2.0 ** -24) + 2.0 ** -22
             # weights: twice that (in the sum and in its normaliser), and 2^-16 for their own two bf16 numbers; partials: half (2^-11)
             dp = 2 * de + 2.0 ** -16
@@ -323,3 +324,45 @@ def test_pages_past_two_to_the_31_bytes():
     lat = np.concatenate([f(pool_c[n16 - 3]), f(pool_c[n16 - 4]), f(src[1])[:5]])
     ro = P.attend(f(q)[0], f(qr)[0], f(w_uk), f(w_uv), lat, np.zeros((len(lat), dr)), 1 / 8)[0]
     assert np.linalg.norm(f(out)[0] - ro) <= 2.0 ** -7 * np.linalg.norm(ro)
+
+
+def test_queries_with_one_large_number_a_block():
+    # the large one meets zeros in the cache, so the logits are what is left of the query beside it.  Its error there: 2^-18.9 of the block's largest times the
+    # sum of the block's magnitudes (four planes of 6-bit floats: steps of 1/2, then 1/4 of a sixteenth, 1/4 of a 2^9th and 1/4 of a 2^14th, half of the last)
+    H, dh, r = 16, 64, 256
+    c = Case(n_heads=H, d_head=dh, r=r, d_rope=32, stride=1, page_slots=16, lens=[200, 48], packed=[12, 3], max_slots=256, spread=2.0, seed=5)
+    c.w_uk[:, ::32, :] *= 512
+    c.pk.tensors["codes"][..., 0] &= 0xf0                                                   # column 0 of every block
+    c.cache_c[..., ::32] = 0
+    c.f64["w_uk"] = c.w_uk.double().cpu().numpy()
+    o, ol, ls = c.run()
+    for b in range(c.batch):
+        lat, key = c.rows[b][0].copy(), c.rows[b][1]
+        lat[:, ::32] = 0
+        ro, rl, rs, bd = P.attend(c.f64["q"][b], c.f64["q_rope"][b], c.f64["w_uk"], c.f64["w_uv"], lat, key, 1 / math.sqrt(dh))
+        qt = np.abs(np.einsum("hk,hrk->hr", c.f64["q"][b], c.f64["w_uk"])).reshape(H, r // 32, 32).max(-1)
+        planes = (qt @ np.abs(lat).reshape(len(lat), r // 32, 32).sum(-1).T).max(-1) * 2.0 ** -18.9 / math.sqrt(dh)
+        de = planes + bd["logit"] * (2.0 ** -16 + (r + 32 + dh) * 2.0 ** -24) + 2.0 ** -22
+        assert np.all(planes < 0.5)
+        assert np.all(np.abs(ls[b] - rs) <= de + 2.0 ** -20 * np.maximum(1, np.abs(rs)))
+        dp = np.exp(2 * de) - 1 + 2.0 ** -16                                                # (a weight and its normaliser)
+        assert np.all(np.abs(ol[b] - rl) <= (dp + 2.0 ** -11)[:, None] * bd["latent"] + 2.0 ** -24)
+
+
+def test_numbers_that_are_none_stay_where_they_are():
+    # a NaN block of a live slot, and a query with an infinity: their sequence (their head) is NaN, the others are what they were
+    c = Case(n_heads=8, d_head=64, r=128, d_rope=32, stride=1, page_slots=16, lens=[100, 90, 64], packed=[6, 5, 4], max_slots=128, seed=9)
+    o, ol, ls = c.check()
+    page = int(c.pk.tensors["table"][0, 2])
+    before = c.pk.tensors["scales"][page, 0, 1, 7].clone()
+    c.pk.tensors["scales"][page, 0, 1, 7] = 255
+    no, nol, nls = c.run()
+    assert np.isnan(no[0]).all() and np.isnan(nls[0]).all()
+    for x, y in ((no, o), (nol, ol), (nls, ls)):
+        assert np.array_equal(x[1:], y[1:])
+    c.pk.tensors["scales"][page, 0, 1, 7] = before
+    c.q[1, 3, 5] = float("inf")
+    no, nol, nls = c.run()
+    assert np.isnan(no[1, 3]).all() and np.isnan(nls[1, 3])
+    keep = [i for i in range(8) if i != 3]
+    assert np.array_equal(no[1, keep], o[1, keep]) and np.array_equal(no[[0, 2]], o[[0, 2]]) and np.array_equal(nls[[0, 2]], ls[[0, 2]])

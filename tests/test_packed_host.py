@@ -199,3 +199,38 @@ def test_reference_tables_are_the_host_books(seed):
         P.fit(mine, None, length, n, page_slots=ps, stride=stride, max_slots=max_slots, keep=0, batch=Bn, n_max=3 * ps)
         length += n
         assert np.array_equal(mine.table, table) and mine.count == book.free_count and mine.head == book.free_head
+
+
+def test_too_many_chunks_of_a_sequence():
+    # 65536 chunks and more do not fit a launch; one slot fewer would
+    a = dict(q=1024, q_rope=1024, w_uk=1024, w_uv=1024, cache_c=1024, cache_kr=1024, seq_len=1024, page_table=1024, packed_cache=packed(max_pages=1), batch=0,
+             out=1024, out_latent=None, lse=None, workspace=1024)
+    ctx = B.Context(**{**PAGED, "max_slots": 32 * 65535 + 1, "stride": 1})
+    args = {**a, "packed_cache": packed(max_pages=-(-(32 * 65535 + 1) // 64)), "batch": 16}
+    ctx.set_decode_chunk(32)
+    assert ctx.decode_attn_packed_status(*args.values()) == B.MTLA_ERR_UNSUPPORTED
+    assert ctx.decode_attn_packed_status(*{**args, "batch": 0}.values()) == BAD
+
+
+CHUNKS = r"""
+#include <cstdio>
+#include "decode_schedule.h"
+int main() {
+  int b, s, h;
+  while (scanf("%d %d %d", &b, &s, &h) == 3) printf("%d\n", mtla::packed_chunk(b, s, h));
+  return 0;
+}
+"""
+
+
+@pytest.mark.skipif(not shutil.which("g++"), reason="no host compiler")
+def test_chunk_rule(tmp_path):
+    (tmp_path / "main.cpp").write_text(CHUNKS)
+    subprocess.run(["g++", "-std=c++17", "-Wall", "-Werror", "-I", CSRC, str(tmp_path / "main.cpp"), "-o", str(tmp_path / "main")], check=True)
+    # the shapes whose times stand beside the rule, then the ends of its range: multiples of 64, 256 of a sequence at most
+    shapes = [(8, 8192, 32), (1, 131071, 16), (256, 2048, 16), (16, 640, 8), (1, 75, 4), (1, 1, 1), (65535, 1, 64), (65535, 32767, 64), (1, (1 << 31) - 1, 16)]
+    run = subprocess.run([str(tmp_path / "main")], input="\n".join("%d %d %d" % s for s in shapes), check=True, capture_output=True, text=True)
+    got = list(map(int, run.stdout.split()))
+    assert got[:5] == [256, 512, 1024, 64, 64]
+    for (b, s, h), c in zip(shapes, got):
+        assert c % 64 == 0 and c >= 64 and -(-s // c) <= 256
