@@ -511,7 +511,7 @@ mtla_status mtla_pages_unpack(mtla_ctx* ctx, void* cache_c, void* cache_kr, cons
  * of their 32 latents' (2^-17 of themselves over bf16 pages): what a query asks of a latent 2^18 times less than of
  * its neighbour is not heard.
  * mtla_set_decode_chunk applies (0: a rule of this call's own, from the context's sequences and heads);
- * mtla_set_decode_schedule does not.  MTLA_ERR_UNSUPPORTED: more than 65535 chunks of max_slots (a small chunk that
+ * mtla_set_decode_schedule does not.  MTLA_ERR_UNSUPPORTED: more than 65534 chunks of max_slots (a small chunk that
  * the caller set), or together with mtla_set_shared_prefix.
  */
 mtla_status mtla_decode_attn_packed(mtla_ctx* ctx, const void* q, const void* q_rope, const void* w_uk, const void* w_uv,

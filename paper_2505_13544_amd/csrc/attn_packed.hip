@@ -3,7 +3,8 @@
 // Eq. (with-rope), incremental case, per tile of 16 slots and 16 heads:
 //     S^T[slot, head] = [C_hat | K_hat^R][slot, :] . [q~ | q^R][head, :]
 //     O^T[col,  head] += C_hat^T[col, slot] . P^T[slot, head]
-// Workgroup = (sequence, 16 heads, chunk of slots).  A wavefront owns 128 latent columns (all 64 at r = 64): CG = r / 128 of them share the slots of a step
+// Workgroup = (sequence, 16 heads, chunk of slots); where the packed slots end inside a chunk, what the chunk holds behind them is another workgroup's (open_piece:
+// in one the open page's two barriers a step came on top, 47 us instead of 43 over 256 lengths from 256 to 2048 slots, 26 instead of 22.7 over 131071).  A wavefront owns 128 latent columns (all 64 at r = 64): CG = r / 128 of them share the slots of a step
 // (64 at r = 512, else 32), and the 4 / CG groups take different slots.  Every byte of the cache is loaded once per 16 heads.
 //   logits   the codes go into the matrix cores as they are: v_mfma_scale_f32_16x16x128_f8f6f4 takes a lane's 32 codes of a slot with the block's power of
 //            two, against the query as four planes of 6-bit floats (E2M3), each with a power of two per 32 columns of a head.  Plane after plane takes what
@@ -19,8 +20,8 @@
 //   512 x 1024 slots (two workgroups a unit)  52 us, 4.0 TB/s: half the time VALU, a quarter MFMA, and the memory (47 us with all pages in L2)
 //   256 x 1024 slots, chunks of 512           33 us, 3.2 TB/s: a step of 64 slots is 1.7 us alone on a unit, 2.4 beside another workgroup's
 //   256 x 32 slots                            9 us: the launch, two reads that wait for each other (0.7 us each, 1.6 with all units reading), an open step (2.3)
-// An equal share of all steps for each of 512 workgroups took 47 us instead of 49 where 256 lengths range from 256 to 2048 slots, and 37 instead of 32 where all are
-// 1024: its scan of the lengths is one more read to wait for.  The open page in front of the packed ones, or its rows asked for ahead of the last step's values: no gain.
+// Tried and left: an equal share of all steps for each of 512 workgroups (ahead of the above 47 us instead of 49 where 256 lengths range from 256 to 2048 slots, but 37
+// instead of 32 where all are 1024: its scan of the lengths is one more read to wait for); the open page in front of the packed ones, its rows asked for early (no gain).
 #include "bounds.h"
 #include "lds_stream.h"
 #include "mtla_device.h"
@@ -667,13 +668,13 @@ __device__ __forceinline__ void stream_open(Worker<C>& w, const Source& s, Chunk
 
 struct Run {  // slots [k0, k1) of sequence b, k0 < k1, k0 a multiple of 16
   int b, k0, k1, piece;
+  int packed;  // the sequence's slots that lie in packed pages
 };
 
 // What a run asks for ahead of everything that it has to know first.
 template <class C>
 struct RunHead {
   PageEntries entries;
-  int n_packed;
   QueryRope<C> qr;
   QueryRows<C> q;
 };
@@ -699,7 +700,6 @@ __device__ __forceinline__ const uint16_t* query_rows(const AttnArgs& at, int b,
 }
 template <class C>
 __device__ __forceinline__ void load_head(RunHead<C>& h, const AttnPackedArgs& a, const Source& s, int b, int k0, const LaneMap<C>& m, int h0, int heads) {
-  h.n_packed = load_uniform_i32(a.pk.n_packed, b);
   h.entries.load(s, k0 >> s.shift, m.lane);
   h.q.load(query_rows<C>(a.at, b, h0), a.at.q_plane, heads, m);
   h.qr.load(query_rows<C>(a.at, b, h0), a.at.q_plane, heads, m);
@@ -710,12 +710,9 @@ __device__ __forceinline__ void attend_run(const AttnPackedArgs& a, const Run& r
   constexpr int R = C::R;
   const AttnArgs& at = a.at;
   const int k0 = run.k0, k1 = run.k1, tid = threadIdx.x, wv = m.wv;
-  int n_packed = head.n_packed;
-  s.n_packed = n_packed = n_packed < 0 ? 0 : (n_packed < at.pages.max_pages ? n_packed : at.pages.max_pages);
   const QueryRope<C>& qr = head.qr;
   Worker<C> w(m, smem);
-  const long long packed_slots = (long long)n_packed << s.shift;
-  const int kp = (int)(packed_slots < k1 ? packed_slots : k1);  // slots below it come out of packed pages
+  const int kp = run.packed < k1 ? run.packed : k1;  // slots below it come out of packed pages
   const int ko = kp > k0 ? kp : k0;
   ChunkPages pages = chunk_pages(head.entries, s, k0 >> s.shift, m.lane);
   if (kp > k0) stream_packed<C>(w, s, pages, head.q, qr, k0, kp);
@@ -801,7 +798,7 @@ __device__ __forceinline__ void attend_run(const AttnPackedArgs& a, const Run& r
   }
 }
 
-// grid = (sequences, tiles of 16 heads, chunks): the head tiles of a chunk run side by side and find its bytes in the caches (32 heads in one workgroup need
+// grid = (sequences, tiles of 16 heads, chunks and the piece behind the packed slots): the head tiles of a chunk run side by side and find its bytes in the caches (32 heads in one workgroup need
 // twice the registers, and few long sequences have too few workgroups); sequences side by side go to different XCDs.
 template <int R, int DR>
 __global__ __launch_bounds__(kBlock, 2) void attn_packed_kernel(AttnPackedArgs a) {
@@ -814,15 +811,35 @@ __global__ __launch_bounds__(kBlock, 2) void attn_packed_kernel(AttnPackedArgs a
   const int heads = at.n_heads - h0 < 16 ? at.n_heads - h0 : 16;
   Run run;
   run.b = blockIdx.x;
-  run.k0 = blockIdx.z * at.chunk;
-  const int len = load_uniform_i32(at.seq_len, run.b);
+  const int len = load_uniform_i32(at.seq_len, run.b), n_packed = load_uniform_i32(a.pk.n_packed, run.b);
+  const bool behind = (int)blockIdx.z == at.n_splits - 1;  // what lies behind the packed slots in their chunk
+  int live = 0;
+  if (behind) {
+    live = live_slots(len, at.stride, at.max_slots);
+    run.packed = packed_slots(n_packed, at.pages.max_pages, at.pages.shift, live);
+    if (!open_piece(run.packed, live, at.chunk)) return;
+    run.k0 = run.packed;
+  } else {
+    run.k0 = blockIdx.z * at.chunk;
+  }
   Source s = source_of<C>(a, run.b);
   RunHead<C> head;
   load_head<C>(head, a, s, run.b, run.k0, m, h0, heads);
-  const int live = live_slots(len, at.stride, at.max_slots);
-  run.k1 = live - run.k0 < at.chunk ? live : run.k0 + at.chunk;
-  run.piece = run.b * at.n_splits + blockIdx.z;
-  if (run.k0 < run.k1) attend_run<C>(a, run, head, s, m, h0, heads, smem);
+  if (behind) {
+    const int chunk_end = at.chunk - run.packed % at.chunk;  // (slots from k0 on)
+    run.k1 = live - run.k0 < chunk_end ? live : run.k0 + chunk_end;
+    run.piece = run.b * at.n_splits + (live + at.chunk - 1) / at.chunk;
+  } else {
+    live = live_slots(len, at.stride, at.max_slots);
+    if (run.k0 >= live) return;
+    run.packed = packed_slots(n_packed, at.pages.max_pages, at.pages.shift, live);
+    run.k1 = live - run.k0 < at.chunk ? live : run.k0 + at.chunk;
+    if (run.packed > run.k0 && run.packed < run.k1) run.k1 = run.packed;
+    run.piece = run.b * at.n_splits + blockIdx.z;
+  }
+  s.n_packed = run.packed >> at.pages.shift;  // (whole pages, or all that live)
+  if (run.packed & ((1 << at.pages.shift) - 1)) ++s.n_packed;
+  attend_run<C>(a, run, head, s, m, h0, heads, smem);
 }
 
 template <int R, int DR>

@@ -10,6 +10,14 @@ namespace mtla {
   return n < max_slots ? n : max_slots;
 }
 
+// Slots of a sequence that lie in packed pages: `n_packed` pages of 2^shift slots, taken as [0, max_pages].
+[[gnu::always_inline]] constexpr int packed_slots(int n_packed, int max_pages, int shift, int live) {
+  const long long end = (long long)(n_packed < 0 ? 0 : (n_packed < max_pages ? n_packed : max_pages)) << shift;
+  return end < live ? (int)end : live;
+}
+// Whether they end inside a chunk: what the chunk holds behind them is a piece of its own then, behind those of the chunks.
+[[gnu::always_inline]] constexpr bool open_piece(int packed, int live, int chunk) { return packed > 0 && packed < live && packed % chunk != 0; }
+
 // May `n` tokens be appended to a sequence of `len`?  0, or the status that refuses them (the sequence is left untouched):
 // 1 (MTLA_ERR_INVALID_ARG) for a length below zero, 3 (MTLA_ERR_CAPACITY) for more than the capacity holds.
 [[gnu::always_inline]] constexpr int append_status(int len, int n, int stride, int max_slots) {

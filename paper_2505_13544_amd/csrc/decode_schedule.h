@@ -12,7 +12,8 @@ constexpr int decode_chunk(int max_batch, int max_slots) {
 }
 
 // The same over packed pages, whose kernel gives every 16 heads workgroups of their own; and no more than 256 chunks of a sequence, which one workgroup a head
-// joins.  us of attention + join at r = 512, chunks of 128 / 256 / 512 / 1024 slots:
+// joins.  us of attention + join at r = 512, chunks of 128 / 256 / 512 / 1024 slots (before the slots behind the packed ones had a workgroup of their own, 43 + 9 and
+// 23 + 14 in the last and the second line since):
 //   8 x 8192, 32 heads     24.8 + 8.9 / 19.6 + 7.0 / 21.4 + 6.3 / 31.3 + 6.5
 //   1 x 131071, 16 heads   26.6 + 38.1 / 22.2 + 21.4 / 27.5 + 13.4 / 38.0 + 9.5
 //   256 x 256 to 2048, 16 heads   82.0 + 14.1 / 65.4 + 11.1 / 57.0 + 9.3 / 51.8 + 8.7

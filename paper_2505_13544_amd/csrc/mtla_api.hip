@@ -48,9 +48,9 @@ constexpr int kMaxPersistent = 1024;
 constexpr int kRunCost = 6;
 constexpr int kBalancedMaxBatch = 2048;  // the running tile counts of a batch live in LDS
 
-// Slots of a chunk over packed pages, and their number.
+// Slots of a chunk over packed pages, and a sequence's pieces: the chunks, and one for what lies behind the packed slots in theirs.
 inline int packed_chunk(const mtla_ctx* c) { return c->chunk_set ? c->chunk : mtla::packed_chunk(c->cfg.max_batch, c->cfg.max_slots, c->cfg.n_heads); }
-inline int packed_splits(const mtla_ctx* c) { return (c->cfg.max_slots + packed_chunk(c) - 1) / packed_chunk(c); }
+inline int packed_splits(const mtla_ctx* c) { return (c->cfg.max_slots + packed_chunk(c) - 1) / packed_chunk(c) + 1; }
 
 // Partials ("pieces") the decode pass can emit: chunks x sequences under the static schedule,
 // one per persistent workgroup plus one per sequence under the balanced one.
@@ -754,6 +754,9 @@ static mtla_status decode_packed_core(mtla_ctx* c, const AppendArgs* ap, const v
   cb.max_slots = g.max_slots;
   cb.chunk = packed_chunk(c);
   cb.n_splits = packed_splits(c);
+  cb.n_packed = pk->n_packed;
+  cb.max_pages = max_pages(g);
+  cb.shift = page_map(c, page_table).shift;
   cb.batch = batch;
   cb.T = 0;
   cb.n_persistent = 0;

@@ -131,6 +131,8 @@ struct CombineArgs {
   int run_cost = 0;             // balanced: units before a row's first tile (as the attention kernel counted)
   int part_f16;                 // part_o holds normalised IEEE-half partials (matrix-core combine only)
   int out_bf16 = 0;             // out is bf16 [rows, n_heads, d_head]
+  const int32_t* n_packed = nullptr;  // chunks over packed pages (open_piece; n_splits counts that piece too)
+  int max_pages = 0, shift = 0;
 };
 
 // Decode attention and value up-projection of whole sequences in one launch (attn_whole.hip).

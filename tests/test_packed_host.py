@@ -202,7 +202,7 @@ def test_reference_tables_are_the_host_books(seed):
 
 
 def test_too_many_chunks_of_a_sequence():
-    # 65536 chunks and more do not fit a launch; one slot fewer would
+    # 65536 pieces and more of a sequence do not fit a launch
     a = dict(q=1024, q_rope=1024, w_uk=1024, w_uv=1024, cache_c=1024, cache_kr=1024, seq_len=1024, page_table=1024, packed_cache=packed(max_pages=1), batch=0,
              out=1024, out_latent=None, lse=None, workspace=1024)
     ctx = B.Context(**{**PAGED, "max_slots": 32 * 65535 + 1, "stride": 1})
