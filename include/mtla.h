@@ -448,7 +448,7 @@ typedef struct {
  * A length may fall, to 0 or by tokens that are dropped, as long as the page it falls into is not a packed one
  * (mtla_pages_unpack first, or keep_pages >= 1).
  *
- *   slot_map   device int64 [batch, n_new_max] or NULL: the row of the pool (page * page_slots + slot in it) that
+ *   slot_map   device int64 [batch, n_new_max] (n_new_max 1 to 2^30) or NULL: the row of the pool (page * page_slots + slot in it) that
  *              token t of sequence b goes to; -1 for padding, beyond the capacity, and for a refused sequence's
  *              tokens without a page
  *   workspace  device, the context's workspace: the status word and, for more than 64 sequences, sums in the place

@@ -682,7 +682,7 @@ mtla_status mtla_pages_fit(mtla_ctx* c, const mtla_page_pool* pool, const mtla_p
   if (!c || !seq_len || !workspace) return MTLA_ERR_INVALID_ARG;
   const mtla_config& g = c->cfg;
   if (g.page_slots <= 0 || batch < 1 || batch > g.max_batch || n_new_max < 0 || keep_pages < 0) return MTLA_ERR_INVALID_ARG;
-  if (slot_map && n_new_max < 1) return MTLA_ERR_INVALID_ARG;
+  if (slot_map && (n_new_max < 1 || n_new_max > 1 << 30)) return MTLA_ERR_INVALID_ARG;
   FitArgs a;
   if (!fit_pool(pool, g.page_slots, a.pool) || (packed && !fit_pool(packed, g.page_slots, a.packed))) return MTLA_ERR_INVALID_ARG;
   if (packed && (packed->table == pool->table || packed->first == pool->first || packed->end == pool->end || packed->ring == pool->ring ||

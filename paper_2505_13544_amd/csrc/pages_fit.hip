@@ -188,6 +188,7 @@ __global__ __launch_bounds__(kBlock) void pages_sums_kernel(FitArgs a, Sums* sum
   }
 }
 
+// Where token `t` behind a sequence's `len` goes in the bf16 pool: entry `k` of its table row (-1: nowhere), and the slot of the page.
 struct TokenPlace {
   int k, in_page;
 };
@@ -199,6 +200,20 @@ __device__ __forceinline__ TokenPlace place_of(const FitArgs& a, int t, int n, i
     if (k >= f && k < e) r = TokenPlace{k, slot & ((1 << a.shift) - 1)};
   }
   return r;
+}
+
+// Rows of four tokens, `step` apart: their table entries are asked for together.
+__device__ __forceinline__ void put_rows(const FitArgs& a, int64_t* out, const int32_t* row, int t0, int step, int n, int len, int f, int e) {
+  TokenPlace to[4];
+  int32_t at[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    to[i] = place_of(a, t0 + i * step, n, len, f, e);
+    at[i] = to[i].k >= 0 ? row[to[i].k] : 0;
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    if (t0 + i * step < a.n_new_max) out[t0 + i * step] = to[i].k >= 0 ? ((int64_t)at[i] << a.shift) + to[i].in_page : -1;
 }
 
 // `sums` (may be NULL: one workgroup): of pages_sums_kernel; `own_map`: a sequence's lane writes its part of the slot map too.
@@ -383,18 +398,7 @@ __global__ __launch_bounds__(kBlock) void pages_fit_kernel(FitArgs a, const Sums
       const int32_t* row = a.pool.table + (size_t)b * P;
       int64_t* out = a.slot_map + (size_t)b * a.n_new_max;
 #pragma unroll 1
-      for (int t0 = 0; t0 < a.n_new_max; t0 += 4) {
-        TokenPlace to[4];
-        int32_t at[4];
-#pragma unroll
-        for (int t = 0; t < 4; ++t) {
-          to[t] = place_of(a, t0 + t, h.n, held.len, nf, ne);
-          at[t] = to[t].k >= 0 ? row[to[t].k] : 0;
-        }
-#pragma unroll
-        for (int t = 0; t < 4; ++t)
-          if (t0 + t < a.n_new_max) out[t0 + t] = to[t].k >= 0 ? ((int64_t)at[t] << a.shift) + to[t].in_page : -1;
-      }
+      for (int t0 = 0; t0 < a.n_new_max; t0 += 4) put_rows(a, out, row, t0, 1, h.n, held.len, nf, ne);
     }
   }
 
@@ -425,10 +429,7 @@ __global__ __launch_bounds__(kBlock) void slot_map_kernel(FitArgs a) {
   const int len = a.seq_len[b], f = a.pool.first[b], e = a.pool.end[b];
   const int32_t* row = a.pool.table + (size_t)b * a.max_pages;
   int64_t* out = a.slot_map + (size_t)b * a.n_new_max;
-  for (int t = blockIdx.x * kBlock + threadIdx.x; t < a.n_new_max; t += gridDim.x * kBlock) {
-    const TokenPlace to = place_of(a, t, n, len, f, e);
-    out[t] = to.k >= 0 ? ((int64_t)row[to.k] << a.shift) + to.in_page : -1;
-  }
+  for (int t = blockIdx.x * 4 * kBlock + threadIdx.x; t < a.n_new_max; t += gridDim.x * 4 * kBlock) put_rows(a, out, row, t, kBlock, n, len, f, e);
 }
 
 }  // namespace

@@ -234,3 +234,10 @@ def test_chunk_rule(tmp_path):
     assert got[:5] == [256, 512, 1024, 64, 64]
     for (b, s, h), c in zip(shapes, got):
         assert c % 64 == 0 and c >= 64 and -(-s // c) <= 256
+
+
+def test_a_slot_map_of_more_tokens_than_an_index_counts():
+    ctx = B.Context(**PAGED)
+    good = dict(pool=pool(), packed=None, seq_len=1024, n_new=None, n_new_max=(1 << 30) + 1, keep_pages=0, batch=16, slot_map=1024, workspace=1024)
+    for n in ((1 << 30) + 1, (1 << 31) - 1):
+        assert _fit(ctx, good, n_new_max=n) == BAD
