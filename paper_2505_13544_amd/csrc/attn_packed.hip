@@ -5,7 +5,7 @@
 //     O^T[col,  head] += C_hat^T[col, slot] . P^T[slot, head]
 // Workgroup = (sequence, 16 heads, chunk of slots); where the packed slots end inside a chunk, what the chunk holds behind them is another workgroup's (open_piece:
 // in one the open page's two barriers a step came on top, 47 us instead of 43 over 256 lengths from 256 to 2048 slots, 26 instead of 22.7 over 131071).  A wavefront owns 128 latent columns (all 64 at r = 64): CG = r / 128 of them share the slots of a step
-// (64 at r = 512, else 32), and the 4 / CG groups take different slots.  Every byte of the cache is loaded once per 16 heads.
+// (64 at r = 512, else 32), and the W / CG groups take different slots (W = 4; 8 for few long sequences at r = 512: packed_wide).  Every byte of the cache is loaded once per 16 heads.
 //   logits   the codes go into the matrix cores as they are: v_mfma_scale_f32_16x16x128_f8f6f4 takes a lane's 32 codes of a slot with the block's power of
 //            two, against the query as four planes of 6-bit floats (E2M3), each with a power of two per 32 columns of a head.  Plane after plane takes what
 //            the ones before left: off by 2^-18 of the block's largest number after four (QueryPlanes).  64 cycles a tile, against 128 for two bf16 planes
@@ -23,6 +23,7 @@
 // Tried and left: an equal share of all steps for each of 512 workgroups (ahead of the above 47 us instead of 49 where 256 lengths range from 256 to 2048 slots, but 37
 // instead of 32 where all are 1024: its scan of the lengths is one more read to wait for); the open page in front of the packed ones, its rows asked for early (no gain).
 #include "bounds.h"
+#include "decode_schedule.h"
 #include "lds_stream.h"
 #include "mtla_device.h"
 #include "packed.h"
@@ -42,16 +43,15 @@ typedef uint32_t u32x6_t __attribute__((ext_vector_type(6)));
 typedef float f32x16_t __attribute__((ext_vector_type(16)));
 typedef float f32x32_t __attribute__((ext_vector_type(32)));
 
-constexpr int kWaves = kBlock / kWave;
 constexpr int kTile = kPackTile;   // slots of an operand tile
 constexpr float kRebase = 40.f;
 
-template <int R_, int DR_>
+template <int R_, int DR_, int W_>
 struct PackCfg {
-  static constexpr int R = R_, DR = DR_;
+  static constexpr int R = R_, DR = DR_, W = W_;      // W wavefronts
   static constexpr int E = R + DR;
   static constexpr int CG = R >= 128 ? R / 128 : 1;   // wavefronts that share a group's slots
-  static constexpr int SG = kWaves / CG;              // groups
+  static constexpr int SG = W / CG;                   // groups
   static constexpr int RW = R / CG;                   // latent columns of a wavefront: 128, or 64
   static constexpr int NB = RW / kPackBlock;          // blocks of a slot: one in each of the lanes g < NB
   static constexpr int DRW = DR / CG;                 // RoPE columns of a wavefront: 8 to 64
@@ -64,15 +64,15 @@ struct PackCfg {
   // a wavefront's rows in LDS: the codes of a step and behind them the scales, in two places, or bf16 rows of two tiles
   static constexpr int tile_bytes = NB * kTile * 16, place_bytes = TL * (tile_bytes + kWave * 4);
   static constexpr int wave_bytes = 2 * place_bytes > 2 * kTile * RW * 2 ? 2 * place_bytes : 2 * kTile * RW * 2;
-  static constexpr size_t park_bytes = (size_t)kWaves * wave_bytes;
+  static constexpr size_t park_bytes = (size_t)W * wave_bytes;
   static constexpr size_t share_bytes = (size_t)SG * TL * (CG - 1) * kWave * 16;            // [group][tile][other wavefront][lane][4 slots]
   static constexpr size_t weight_bytes = CG > 1 ? (size_t)SG * TL * kWave * 16 : 0;         // [group][pair of tiles][plane][lane][4 slots of either tile]
   static constexpr size_t loop_bytes = park_bytes + 2 * share_bytes + 2 * weight_bytes;
   static constexpr int OS = R + 4;                                                          // row stride of the groups' sums when they are merged (floats)
   static constexpr size_t merge_bytes = SG > 1 ? (size_t)SG * 16 * OS * 4 : 0;
   static constexpr size_t body_bytes = loop_bytes > merge_bytes ? loop_bytes : merge_bytes;
-  static constexpr size_t top_bytes = (size_t)kWaves * 16 * 4;                              // [wavefront][head]
-  static constexpr size_t lds_bytes = body_bytes + 2 * top_bytes + 2 * kWaves * 4;          // and whether a wavefront's weights need another reference
+  static constexpr size_t top_bytes = (size_t)W * 16 * 4;                              // [wavefront][head]
+  static constexpr size_t lds_bytes = body_bytes + 2 * top_bytes + 2 * W * 4;          // and whether a wavefront's weights need another reference
 };
 
 // Where a wavefront's and a lane's part of everything is: constant for the kernel.
@@ -293,7 +293,7 @@ struct Worker {
     return reinterpret_cast<u32x4_t*>(smem + C::park_bytes + 2 * C::share_bytes + par * C::weight_bytes) + m.sg * TL * kWave + m.lane;
   }
   __device__ __forceinline__ float* tops() const { return reinterpret_cast<float*>(smem + C::body_bytes); }
-  __device__ __forceinline__ int* flags(int par) const { return reinterpret_cast<int*>(smem + C::body_bytes + 2 * C::top_bytes) + par * kWaves; }
+  __device__ __forceinline__ int* flags(int par) const { return reinterpret_cast<int*>(smem + C::body_bytes + 2 * C::top_bytes) + par * C::W; }
 
   __device__ __forceinline__ void barrier() const {  // of the wavefronts that share slots
     if constexpr (CG > 1) __syncthreads();
@@ -366,7 +366,9 @@ struct Worker {
   }
   __device__ __forceinline__ int any_flag(int par) const {
     if constexpr (CG == 1) return 0;
-    const int4 f = *reinterpret_cast<const int4*>(flags(par));
+    const int4* at = reinterpret_cast<const int4*>(flags(par));
+    int4 f = at[0];
+    if constexpr (C::W == 8) f = make_int4(f.x | at[1].x, f.y | at[1].y, f.z | at[1].z, f.w | at[1].w);
     return f.x | f.y | f.z | f.w;
   }
 
@@ -725,7 +727,7 @@ __device__ __forceinline__ void attend_run(const AttnPackedArgs& a, const Run& r
 
   // ---- normalisers and references of the groups
   float* part_l = w.tops();                              // [wavefront][head]
-  float* refs = part_l + kWaves * 16;                    // [group][head]
+  float* refs = part_l + C::W * 16;                    // [group][head]
   w.barrier();  // (the tops' place may have been in use)
   const float l_wave = quarter_reduce(w.l_run, LaneSum());
   if (m.g == 0) part_l[wv * 16 + m.l16] = l_wave;
@@ -770,7 +772,7 @@ __device__ __forceinline__ void attend_run(const AttnPackedArgs& a, const Run& r
     }
     __syncthreads();
     constexpr int R4 = R / 4;
-    for (int i = tid; i < heads * R4; i += kBlock) {
+    for (int i = tid; i < heads * R4; i += C::W * kWave) {
       const int h = i / R4, c4 = i - h * R4;
       float ref[C::SG], top = -INFINITY, l = 0.f;
 #pragma unroll
@@ -800,9 +802,9 @@ __device__ __forceinline__ void attend_run(const AttnPackedArgs& a, const Run& r
 
 // grid = (sequences, tiles of 16 heads, chunks and the piece behind the packed slots): the head tiles of a chunk run side by side and find its bytes in the caches (32 heads in one workgroup need
 // twice the registers, and few long sequences have too few workgroups); sequences side by side go to different XCDs.
-template <int R, int DR>
-__global__ __launch_bounds__(kBlock, 2) void attn_packed_kernel(AttnPackedArgs a) {
-  using C = PackCfg<R, DR>;
+template <int R, int DR, int W>
+__global__ __launch_bounds__(W * kWave, 2) void attn_packed_kernel(AttnPackedArgs a) {
+  using C = PackCfg<R, DR, W>;
   extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
   const int tid = threadIdx.x, lane = tid & (kWave - 1), h0 = blockIdx.y * 16;
   const int wv = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -842,23 +844,25 @@ __global__ __launch_bounds__(kBlock, 2) void attn_packed_kernel(AttnPackedArgs a
   attend_run<C>(a, run, head, s, m, h0, heads, smem);
 }
 
-template <int R, int DR>
+template <int R, int DR, int W>
 hipError_t launch_one(const AttnPackedArgs& a, hipStream_t st, const EventPair& ev) {
-  using C = PackCfg<R, DR>;
+  using C = PackCfg<R, DR, W>;
   static DeviceSet lds_allowed;
-  const hipError_t e = allow_lds(&attn_packed_kernel<R, DR>, C::lds_bytes, lds_allowed);
+  const hipError_t e = allow_lds(&attn_packed_kernel<R, DR, W>, C::lds_bytes, lds_allowed);
   if (e != hipSuccess) return e;
   const dim3 grid(a.at.batch, (a.at.n_heads + 15) / 16, a.at.n_splits);
-  launch_timed(attn_packed_kernel<R, DR>, grid, dim3(kBlock), C::lds_bytes, st, ev, a);
+  launch_timed(attn_packed_kernel<R, DR, W>, grid, dim3(W * kWave), C::lds_bytes, st, ev, a);
   return hipGetLastError();
 }
 
 }  // namespace
 
 hipError_t launch_attn_packed(const AttnPackedArgs& a, hipStream_t st, const EventPair& ev) {
+  if (a.at.r == 512 && packed_wide(a.at.r, a.at.batch, a.at.n_heads, a.at.n_splits - 1, a.at.chunk))
+    return a.at.d_rope == 32 ? launch_one<512, 32, 8>(a, st, ev) : launch_one<512, 64, 8>(a, st, ev);
 #define MTLA_CASE(RR, DD)                       \
   if (a.at.r == RR && a.at.d_rope == DD)        \
-    return launch_one<RR, DD>(a, st, ev);
+    return launch_one<RR, DD, 4>(a, st, ev);
   MTLA_CASE(64, 32)
   MTLA_CASE(64, 64)
   MTLA_CASE(128, 32)

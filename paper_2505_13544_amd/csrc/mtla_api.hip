@@ -49,7 +49,7 @@ constexpr int kRunCost = 6;
 constexpr int kBalancedMaxBatch = 2048;  // the running tile counts of a batch live in LDS
 
 // Slots of a chunk over packed pages, and a sequence's pieces: the chunks, and one for what lies behind the packed slots in theirs.
-inline int packed_chunk(const mtla_ctx* c) { return c->chunk_set ? c->chunk : mtla::packed_chunk(c->cfg.max_batch, c->cfg.max_slots, c->cfg.n_heads); }
+inline int packed_chunk(const mtla_ctx* c) { return c->chunk_set ? c->chunk : mtla::packed_chunk(c->cfg.r, c->cfg.max_batch, c->cfg.max_slots, c->cfg.n_heads); }
 inline int packed_splits(const mtla_ctx* c) { return (c->cfg.max_slots + packed_chunk(c) - 1) / packed_chunk(c) + 1; }
 
 // Partials ("pieces") the decode pass can emit: chunks x sequences under the static schedule,

@@ -366,3 +366,16 @@ def test_numbers_that_are_none_stay_where_they_are():
     assert np.isnan(no[1, 3]).all() and np.isnan(nls[1, 3])
     keep = [i for i in range(8) if i != 3]
     assert np.array_equal(no[1, keep], o[1, keep]) and np.array_equal(no[[0, 2]], o[[0, 2]]) and np.array_equal(nls[[0, 2]], ls[[0, 2]])
+
+
+@pytest.mark.parametrize("chunk", [256, 288, 1024])
+@pytest.mark.parametrize("n_heads,d_rope,page_slots,slots,packed", [
+    (16, 64, 16, [3000], [187]), (20, 32, 64, [1025, 40], [16, 0]), (5, 64, 32, [64, 0, 2047, 129], [2, 0, 40, 4]), (64, 32, 16, [700], [0]), (33, 64, 128, [1900], [14])])
+def test_few_long_sequences_in_wide_workgroups(n_heads, d_rope, page_slots, slots, packed, chunk):
+    # up to four groups of heads and sequences at r = 512, chunks of 256 slots and more: eight wavefronts, two groups of them, of which one may have no slot
+    Case(n_heads=n_heads, d_head=64, r=512, d_rope=d_rope, stride=1, page_slots=page_slots, lens=slots, packed=packed, max_slots=3001, chunk=chunk, seed=n_heads).check()
+
+
+def test_a_reference_that_moves_in_wide_workgroups():
+    for spread in (0.0, 60.0):
+        Case(n_heads=16, d_head=64, r=512, d_rope=32, stride=1, page_slots=16, lens=[900, 70], packed=[50, 4], max_slots=1024, spread=spread, chunk=512).check(f"spread {spread}")

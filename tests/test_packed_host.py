@@ -216,8 +216,11 @@ CHUNKS = r"""
 #include <cstdio>
 #include "decode_schedule.h"
 int main() {
-  int b, s, h;
-  while (scanf("%d %d %d", &b, &s, &h) == 3) printf("%d\n", mtla::packed_chunk(b, s, h));
+  int r, b, s, h;
+  while (scanf("%d %d %d %d", &r, &b, &s, &h) == 4) {
+    const int c = mtla::packed_chunk(r, b, s, h);
+    printf("%d %d\n", c, (int)mtla::packed_wide(r, b, h, (s + c - 1) / c, c));
+  }
   return 0;
 }
 """
@@ -227,13 +230,17 @@ int main() {
 def test_chunk_rule(tmp_path):
     (tmp_path / "main.cpp").write_text(CHUNKS)
     subprocess.run(["g++", "-std=c++17", "-Wall", "-Werror", "-I", CSRC, str(tmp_path / "main.cpp"), "-o", str(tmp_path / "main")], check=True)
-    # the shapes whose times stand beside the rule, then the ends of its range: multiples of 64, 256 of a sequence at most
-    shapes = [(8, 8192, 32), (1, 131071, 16), (256, 2048, 16), (16, 640, 8), (1, 75, 4), (1, 1, 1), (65535, 1, 64), (65535, 32767, 64), (1, (1 << 31) - 1, 16)]
-    run = subprocess.run([str(tmp_path / "main")], input="\n".join("%d %d %d" % s for s in shapes), check=True, capture_output=True, text=True)
-    got = list(map(int, run.stdout.split()))
-    assert got[:5] == [256, 512, 1024, 64, 64]
-    for (b, s, h), c in zip(shapes, got):
-        assert c % 64 == 0 and c >= 64 and -(-s // c) <= 256
+    # the shapes whose times stand beside the rule, then the ends of its range: multiples of 64, 256 of a sequence at most, wide ones on 256 units at most
+    shapes = [(512, 8, 8192, 32), (512, 1, 131071, 16), (512, 256, 2048, 16), (256, 16, 640, 8), (64, 1, 75, 4), (512, 1, 65536, 16), (512, 1, 131071, 32),
+              (512, 1, 32768, 16), (256, 1, 131071, 16)]
+    ends = [(512, 1, 1, 1), (64, 65535, 1, 64), (64, 65535, 32767, 64)] + [(512, b, s, 16) for b in (1, 2, 3, 4, 5) for s in (65535, 65536, 99999, (1 << 31) - 1)]
+    run = subprocess.run([str(tmp_path / "main")], input="\n".join("%d %d %d %d" % s for s in shapes + ends), check=True, capture_output=True, text=True)
+    got = np.array(run.stdout.split(), int).reshape(-1, 2)
+    assert got[:9].tolist() == [[256, 0], [576, 1], [1024, 0], [64, 0], [64, 0], [512, 1], [1088, 1], [192, 0], [512, 0]]
+    for (r, b, s, h), (c, wide) in zip(shapes + ends, got):
+        chunks = -(-s // c)
+        assert c % 64 == 0 and c >= 64 and chunks <= 256
+        assert not wide or b * -(-h // 16) * (chunks + 1) <= 256
 
 
 def test_a_slot_map_of_more_tokens_than_an_index_counts():
