@@ -4,8 +4,9 @@
 //     S^T[slot, head] = [C_hat | K_hat^R][slot, :] . [q~ | q^R][head, :]
 //     O^T[col,  head] += C_hat^T[col, slot] . P^T[slot, head]
 // Workgroup = (sequence, 16 heads, chunk of slots); where the packed slots end inside a chunk, what the chunk holds behind them is another workgroup's (open_piece:
-// in one the open page's two barriers a step came on top, 47 us instead of 43 over 256 lengths from 256 to 2048 slots, 26 instead of 22.7 over 131071).  A wavefront owns 128 latent columns (all 64 at r = 64): CG = r / 128 of them share the slots of a step
-// (64 at r = 512, else 32), and the W / CG groups take different slots (W = 4; 8 for few long sequences at r = 512: packed_wide).  Every byte of the cache is loaded once per 16 heads.
+// in one the open page's two barriers a step came on top, 47 us instead of 43 over 256 lengths from 256 to 2048 slots, 26 instead of 22.7 over 131071).
+// A wavefront owns 128 latent columns (all 64 at r = 64): CG = r / 128 of them share the slots of a step (64 at r = 512, else 32), and the W / CG groups take
+// different slots (W = 4; 8 for few long sequences at r = 512: packed_wide).  Every byte of the cache is loaded once per 16 heads.
 //   logits   the codes go into the matrix cores as they are: v_mfma_scale_f32_16x16x128_f8f6f4 takes a lane's 32 codes of a slot with the block's power of
 //            two, against the query as four planes of 6-bit floats (E2M3), each with a power of two per 32 columns of a head.  Plane after plane takes what
 //            the ones before left: off by 2^-18 of the block's largest number after four (QueryPlanes).  64 cycles a tile, against 128 for two bf16 planes
@@ -71,8 +72,8 @@ struct PackCfg {
   static constexpr int OS = R + 4;                                                          // row stride of the groups' sums when they are merged (floats)
   static constexpr size_t merge_bytes = SG > 1 ? (size_t)SG * 16 * OS * 4 : 0;
   static constexpr size_t body_bytes = loop_bytes > merge_bytes ? loop_bytes : merge_bytes;
-  static constexpr size_t top_bytes = (size_t)W * 16 * 4;                              // [wavefront][head]
-  static constexpr size_t lds_bytes = body_bytes + 2 * top_bytes + 2 * W * 4;          // and whether a wavefront's weights need another reference
+  static constexpr size_t top_bytes = (size_t)W * 16 * 4;                                   // [wavefront][head]
+  static constexpr size_t lds_bytes = body_bytes + 2 * top_bytes + 2 * W * 4;               // and whether a wavefront's weights need another reference
 };
 
 // Where a wavefront's and a lane's part of everything is: constant for the kernel.
@@ -726,7 +727,7 @@ __device__ __forceinline__ void attend_run(const AttnPackedArgs& a, const Run& r
   }
 
   // ---- normalisers and references of the groups
-  float* part_l = w.tops();                              // [wavefront][head]
+  float* part_l = w.tops();                            // [wavefront][head]
   float* refs = part_l + C::W * 16;                    // [group][head]
   w.barrier();  // (the tops' place may have been in use)
   const float l_wave = quarter_reduce(w.l_run, LaneSum());
@@ -800,8 +801,8 @@ __device__ __forceinline__ void attend_run(const AttnPackedArgs& a, const Run& r
   }
 }
 
-// grid = (sequences, tiles of 16 heads, chunks and the piece behind the packed slots): the head tiles of a chunk run side by side and find its bytes in the caches (32 heads in one workgroup need
-// twice the registers, and few long sequences have too few workgroups); sequences side by side go to different XCDs.
+// grid = (sequences, tiles of 16 heads, chunks and the piece behind the packed slots): the head tiles of a chunk run side by side and find its bytes in the
+// caches (32 heads in one workgroup need twice the registers, and few long sequences have too few workgroups); sequences side by side go to different XCDs.
 template <int R, int DR, int W>
 __global__ __launch_bounds__(W * kWave, 2) void attn_packed_kernel(AttnPackedArgs a) {
   using C = PackCfg<R, DR, W>;

@@ -12,15 +12,16 @@ constexpr int decode_chunk(int max_batch, int max_slots) {
 }
 
 // The same over packed pages, whose kernel gives every 16 heads workgroups of their own; and no more than 256 chunks of a sequence, which one workgroup a head
-// joins.  us of attention + join at r = 512, chunks of 128 / 256 / 512 / 1024 slots (before the slots behind the packed ones had a workgroup of their own, 43 + 9 and
-// 23 + 14 in the last and the second line since):
-//   8 x 8192, 32 heads     24.8 + 8.9 / 19.6 + 7.0 / 21.4 + 6.3 / 31.3 + 6.5
-//   1 x 131071, 16 heads   26.6 + 38.1 / 22.2 + 21.4 / 27.5 + 13.4 / 38.0 + 9.5
-//   256 x 256 to 2048, 16 heads   82.0 + 14.1 / 65.4 + 11.1 / 57.0 + 9.3 / 51.8 + 8.7
-// At r = 512 up to four of these groups of heads and sequences take workgroups of eight wavefronts (packed_wide), one a unit, in chunks that leave room for the pieces
-// behind the packed slots: as many steps side by side on a unit as two workgroups of four, and half of the pieces.  us, attention + join, wide / the best of the above:
-//   16 heads, 1 x 131071  22.6 + 12.5 / 23.6 + 14.1, 1 x 65536 (chunks of 512) 17.9 + 9.3 / 15.8 + 13.8, 2 x 131071 32.0 + 10.1 / 36.3 + 10.2, 4 x 131071 52.0 + 8.8 / 57.3 +
-//   10.5, 4 x 32768 21.8 + 7.6 / 22.5 + 8.4; 32 heads, 1 x 131071 30.3 + 9.8 / 35.6 + 10.2, but 8 x 8192 19.8 + 6.8 / 18.9 + 6.9
+// joins.  us of attention + join at r = 512, chunks of 128 / 256 / 512 / 1024 slots:
+//   8 x 8192, 32 heads            24.7 + 9.2 / 19.8 + 7.2 / 20.6 + 7.0 / 30.2 + 6.8
+//   256 x 256 to 2048, 16 heads   78.0 + 14.6 / 59.5 + 11.6 / 49.8 + 10.0 / 45.4 + 9.0
+//   1 x 131071, 16 heads          25.4 + 38.1 / 23.8 + 21.9 / 23.6 + 14.1 (four wavefronts)
+// At r = 512 up to four of these groups of heads and sequences take workgroups of eight wavefronts (packed_wide), one a unit, in chunks that leave room for the
+// pieces behind the packed slots: as many steps side by side on a unit as two workgroups of four, and half of the pieces.  us, attention + join, wide / the best
+// of four wavefronts:
+//   16 heads   1 x 131071 22.6 + 12.5 / 23.6 + 14.1, 1 x 65536 (chunks of 512) 17.9 + 9.3 / 15.8 + 13.8, 2 x 131071 32.0 + 10.1 / 36.3 + 10.2,
+//              4 x 131071 52.0 + 8.8 / 57.3 + 10.5, 4 x 32768 21.8 + 7.6 / 22.5 + 8.4
+//   32 heads   1 x 131071 30.3 + 9.8 / 35.6 + 10.2, but 8 x 8192 19.8 + 6.8 / 18.9 + 6.9
 constexpr int packed_chunk(int r, int max_batch, int max_slots, int n_heads) {
   const int groups = max_batch * ((n_heads + 15) / 16);
   if (r == 512 && groups <= 4) {
