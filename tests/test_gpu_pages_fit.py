@@ -169,7 +169,7 @@ def test_words_that_hold_anything_stay_inside_the_arrays():
     for word in (-(1 << 31), -1, 3, 100, (1 << 31) - 1):
         arena = torch.full((4096,), -5, dtype=torch.int32, device=DEV)
         part = lambda at, *shape: arena[at:at + int(np.prod(shape))].view(*shape)
-        t = dict(table=part(512, n, mp), first=part(1024, n), end=part(1536, n), ring=part(2048, pages), state=part(2560, 4), was_end=part(3072, n))
+        t = dict(table=part(512, n, mp), first=part(1024, n), end=part(1536, n), ring=part(2048, pages), state=part(2560, 4), was_end=part(3200, n))
         for k, v in t.items():
             v.copy_(dev(rng.integers(0, pages, v.shape).astype(np.int32)))
         t["state"][0], t["state"][1] = word, word
@@ -177,7 +177,7 @@ def test_words_that_hold_anything_stay_inside_the_arrays():
         ctx.pages_fit(B.PagePool(**t), None, dev(np.array([60, 1, 0, 64, 33, 2], np.int32)), None, 4, 0, n, None, ws, torch.cuda.current_stream().cuda_stream)
         ctx.device_status(ws, torch.cuda.current_stream().cuda_stream)
         inside = torch.zeros(4096, dtype=torch.bool, device=DEV)
-        for at, size in ((512, n * mp), (1024, n), (1536, n), (2048, pages), (2560, 4), (3072, n)):
+        for at, size in ((512, n * mp), (1024, n), (1536, n), (2048, pages), (2560, 4), (3200, n)):
             inside[at:at + size] = True
         assert bool((arena[~inside] == -5).all()), word
         assert 0 <= int(t["state"][0]) < pages and 0 <= int(t["state"][1]) <= pages
