@@ -506,7 +506,8 @@ mtla_status mtla_pages_unpack(mtla_ctx* ctx, void* cache_c, void* cache_kr, cons
  * step appends through page_table, so the page that its token goes to must not be a packed one (mtla_pages_fit
  * sees to that).  Arguments, checks and errors as there, any n_heads and d_head, but
  *   out   device elem [batch, n_heads, d_head] or NULL: bf16, what W_O's product takes; its rounding is the largest
- *         error behind the packing (sums, weights and normalisers are fp32 or better than 16 bits)
+ *         error behind the packing (sums, normalisers and the chunks' partials are fp32; weights, the absorbed query
+ *         and, in front of the value projection, the latent output are two bf16 numbers each, off by 2^-17)
  * A head's absorbed query enters the products with the codes as numbers that are off by at most 2^-18 of the largest
  * of their 32 latents' (2^-17 of themselves over bf16 pages): what a query asks of a latent 2^18 times less than of
  * its neighbour is not heard.

@@ -15,7 +15,8 @@
 //   values   the codes go through the wavefront's own LDS as they are and come back transposed by bytes; behind that they become bf16 pairs and operands.
 //            Converted first, as bf16 rows, they were four times the bytes there: of a step's 1900 cycles LDS was busy with 960 (13 a 16-byte store of a wavefront).
 // The packed cache is a third of the bytes of the bf16 one, so the matrix cores have time for the second plane of the weights: the output's error is its own
-// rounding to bf16 (one plane would add as much again).  The normaliser sums the unrounded weights.
+// rounding to bf16 (one plane would add as much again).  The normaliser sums the unrounded weights, and the chunks' sums meet as fp32: latents reach from 2^-124
+// to 6 x 2^125, and a half, for all that it is half the bytes to join, holds 11 bits of numbers from 2^-14 to 65504.
 //
 // Between two barriers a wavefront forms the values of step i - 1, the weights of step i and the logits of step i + 1.  What bounds it, r = 512, 16 heads:
 //   512 x 1024 slots (two workgroups a unit)  52 us, 4.0 TB/s: half the time VALU, a quarter MFMA, and the memory (47 us with all pages in L2)
@@ -742,21 +743,11 @@ __device__ __forceinline__ void attend_run(const AttnPackedArgs& a, const Run& r
     for (int cg = 0; cg < C::CG; ++cg) l += part_l[cg * 16 + m.l16];
     if (m.l16 < heads) {
       const size_t oh = piece * at.n_heads + h0 + m.l16, col = oh * R + m.cg * C::RW + 8 * m.g;
-      if (at.part_f16) {
-        const float inv = 1.f / l;
-        uint16_t* po = reinterpret_cast<uint16_t*>(at.part_o) + col;
 #pragma unroll
-        for (int nb = 0; nb < C::NB; ++nb) {
-          const float4_t a0 = w.o[2 * nb] * inv, a1 = w.o[2 * nb + 1] * inv;
-          *reinterpret_cast<uint4*>(po + 32 * nb) = make_uint4(pack_f16x2(a0[0], a1[0]), pack_f16x2(a0[1], a1[1]), pack_f16x2(a0[2], a1[2]), pack_f16x2(a0[3], a1[3]));
-        }
-      } else {
-#pragma unroll
-        for (int nb = 0; nb < C::NB; ++nb) {
-          const float4_t a0 = w.o[2 * nb], a1 = w.o[2 * nb + 1];
-          *reinterpret_cast<float4_t*>(at.part_o + col + 32 * nb) = float4_t{a0[0], a1[0], a0[1], a1[1]};
-          *reinterpret_cast<float4_t*>(at.part_o + col + 32 * nb + 4) = float4_t{a0[2], a1[2], a0[3], a1[3]};
-        }
+      for (int nb = 0; nb < C::NB; ++nb) {
+        const float4_t a0 = w.o[2 * nb], a1 = w.o[2 * nb + 1];
+        *reinterpret_cast<float4_t*>(at.part_o + col + 32 * nb) = float4_t{a0[0], a1[0], a0[1], a1[1]};
+        *reinterpret_cast<float4_t*>(at.part_o + col + 32 * nb + 4) = float4_t{a0[2], a1[2], a0[3], a1[3]};
       }
       if (wv == 0 && m.g == 0) *reinterpret_cast<float2*>(at.part_ml + oh * 2) = make_float2(w.m_ref, l);
     }
@@ -790,12 +781,7 @@ __device__ __forceinline__ void attend_run(const AttnPackedArgs& a, const Run& r
         for (int cg = 0; cg < C::CG; ++cg) l += f * part_l[(sg * C::CG + cg) * 16 + h];
       }
       const size_t oh = piece * at.n_heads + h0 + h, col = oh * R + 4 * c4;
-      if (at.part_f16) {
-        const float inv = 1.f / l;
-        *reinterpret_cast<uint2*>(reinterpret_cast<uint16_t*>(at.part_o) + col) = make_uint2(pack_f16x2(sum[0] * inv, sum[1] * inv), pack_f16x2(sum[2] * inv, sum[3] * inv));
-      } else {
-        *reinterpret_cast<float4_t*>(at.part_o + col) = sum;
-      }
+      *reinterpret_cast<float4_t*>(at.part_o + col) = sum;
       if (c4 == 0) *reinterpret_cast<float2*>(at.part_ml + oh * 2) = make_float2(top, l);
     }
   }

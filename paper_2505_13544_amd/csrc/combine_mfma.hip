@@ -339,8 +339,7 @@ hipError_t launch_rdh_pf(const CombineArgs& a, hipStream_t st) {
   const int rows = a.T ? a.batch * a.T : a.batch;
   // a handful of rows of eight or more pieces each (balanced: at most n_persistent + rows pieces exist): one row per
   // workgroup, its pieces split over the wavefronts
-  // (likewise chunks over packed pages: one sequence of 128 pieces, 16 heads, r = 512 in four rows a workgroup 48 us)
-  if (PF16 && (a.n_persistent > 0 ? rows <= 16 && a.n_persistent + rows >= 8 * rows : rows * a.n_heads <= 256 && a.n_splits >= 8))
+  if (PF16 && a.n_persistent > 0 && rows <= 16 && a.n_persistent + rows >= 8 * rows)
     return launch_one<R, DH, 1, PF16, true>(a, dim3(a.n_heads, rows), 1, st);
   // a small decode step, at most one (row, head) per compute unit, where a row is long (r = 512) or its pieces are more
   // than one round of requests: likewise.  With four rows per workgroup 4 sequences of 32 pieces, 16 heads, r = 512 took

@@ -761,7 +761,7 @@ static mtla_status decode_packed_core(mtla_ctx* c, const AppendArgs* ap, const v
   cb.T = 0;
   cb.n_persistent = 0;
   cb.tile_prefix = nullptr;
-  cb.part_f16 = combine_mfma_supported(cb) ? 1 : 0;
+  cb.part_f16 = 0;
 
   AttnPackedArgs a;
   AttnArgs& at = a.at;
@@ -783,7 +783,7 @@ static mtla_status decode_packed_core(mtla_ctx* c, const AppendArgs* ap, const v
   at.T = 0;
   at.n_persistent = 0;
   at.tile_prefix = nullptr;
-  at.part_f16 = cb.part_f16;
+  at.part_f16 = 0;
   at.pages = page_map(c, page_table);
   a.pk = packed_map(*pk);
 

@@ -1,0 +1,58 @@
+"""GPU tests of what the attention over packed pages keeps of its sums: between the chunks of a sequence they are single precision, with its range.  Inputs
+for which every product and sum is exact in 24 bits, and inputs that differ by a power of two alone, whose results then do too."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from tests.test_gpu_packed import Case
+
+pytestmark = pytest.mark.gpu
+
+# n_heads, d_head, r, slots, packed pages, chunk (0: the call's own); pages of 16 slots
+SHAPES = [(4, 64, 64, [75, 16, 0, 5], [4, 1, 0, 0], 0), (20, 64, 128, [300, 33], [18, 1], 64), (8, 128, 256, [300, 200, 17], [18, 12, 1], 0),
+          (16, 128, 512, [300, 64, 129, 31, 90], [18, 4, 8, 1, 0], 96), (16, 64, 512, [700], [43], 256), (12, 96, 128, [300, 33], [18, 2], 64),
+          (16, 64, 64, [300] * 20, [18] * 20, 32)]
+
+
+def case(n_heads, d_head, r, slots, packed, chunk, **kw):
+    return Case(n_heads=n_heads, d_head=d_head, r=r, d_rope=32, stride=1, page_slots=16, lens=slots, packed=packed, max_slots=max(slots) + 20, chunk=chunk,
+                seed=r + n_heads, **kw)
+
+
+@pytest.mark.parametrize("n_heads,d_head,r,slots,packed,chunk", SHAPES)
+def test_the_mean_of_exact_numbers(n_heads, d_head, r, slots, packed, chunk):
+    # a query of zeros gives every slot the weight 1; the latents are multiples of 2^-5 below 8, not negative, so their sums over 700 slots are exact in
+    # fp32 (18 bits).  What is left is the division: a reciprocal and a product, a step each at most
+    c = case(n_heads, d_head, r, slots, packed, chunk)
+    c.q.zero_(), c.q_rope.zero_()
+    c.pk.tensors["codes"] &= 0x77
+    nan = torch.isnan(c.cache_c)
+    c.cache_c.copy_(torch.where(nan, c.cache_c.float(), (c.cache_c.float().abs().clamp(max=7.0) * 32).round() / 32).bfloat16())
+    o, ol, ls = c.run()
+    for b, n in enumerate(slots):
+        if n == 0:
+            assert not ol[b].any()
+            continue
+        lat = np.abs(c.rows[b][0])
+        n4 = min(packed[b] * 16, n)
+        lat[n4:] = np.round(np.minimum(lat[n4:], 7.0) * 32) / 32
+        mean = lat.sum(0) / n
+        assert np.all(np.abs(ol[b] - mean) <= 2.0 ** -22 * mean), f"sequence {b}: {(np.abs(ol[b] - mean) / np.maximum(mean, 1e-9)).max()}"
+        assert np.all(np.abs(ls[b] - math.log(n)) <= 2.0 ** -20 * max(1.0, math.log(n)))
+
+
+@pytest.mark.parametrize("power", [20, -20, 60, -60])
+@pytest.mark.parametrize("n_heads,d_head,r,slots,packed,chunk", SHAPES)
+def test_latents_of_any_size(n_heads, d_head, r, slots, packed, chunk, power):
+    # latents times 2^k and queries (not their RoPE part) times 2^-k: the same logits and weights, and outputs times 2^k, bit for bit
+    c = case(n_heads, d_head, r, slots, packed, chunk, spread=2.0)
+    o, ol, ls = c.check()
+    c.q.mul_(2.0 ** -power)
+    c.cache_c.mul_(2.0 ** power)
+    scales = c.pk.tensors["scales"]
+    scales.copy_(torch.where(scales == 255, scales, scales + power if power > 0 else scales - (-power)))
+    no, nol, nls = c.run()
+    assert np.array_equal(nls, ls)
+    assert np.array_equal(nol, np.ldexp(ol, power)) and np.array_equal(no, np.ldexp(o, power))
