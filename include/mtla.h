@@ -446,7 +446,9 @@ typedef struct {
  * page for its new tokens; with spill >= 0 its missing entries name that page, so that an append that nobody
  * held back writes there and not into another sequence's page.
  * A length may fall, to 0 or by tokens that are dropped, as long as the page it falls into is not a packed one
- * (mtla_pages_unpack first, or keep_pages >= 1).
+ * (mtla_pages_unpack first, or keep_pages >= 1).  A call without `packed` leaves the packed pages of its sequences as
+ * they are, also those of a sequence that was released and of tokens that were dropped: fit both pools to the lengths
+ * before it, and before mtla_pages_unpack.
  *
  *   slot_map   device int64 [batch, n_new_max] (n_new_max 1 to 2^30) or NULL: the row of the pool (page * page_slots + slot in it) that
  *              token t of sequence b goes to; -1 for padding, beyond the capacity, and for a refused sequence's

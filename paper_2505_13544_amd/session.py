@@ -506,11 +506,13 @@ class PackedSession:
     def unpack(self, batch: int, n_new: int = 0, *, counts=None, slot_map=None, at: int = 0):
         """The sequences in bf16 pages alone, with room for n_new more tokens: what a prefill that continues them reads.  Their packed pages
         stay as they are; the next fit gives the bf16 ones back."""
+        # both pools as the lengths are now: a row released since, or cut short, has packed pages that are not its tokens'
+        self.fit(batch, at=at)
         pool, packed, cache = self._part(at)
         self.ctx.pages_fit(pool, None, self.seq_len[at:], counts, n_new, 0, batch, slot_map, self.workspace, self.stream)
-        # (a sequence that got no pages holds none below its first: none of another's is written)
-        self.ctx.pages_unpack(self.pool_c, self.pool_kr, pool.tensors["table"], cache, pool.tensors["first"], packed.tensors["end"], batch,
-                              self.max_pages, self.stream)
+        # a sequence that got no pages holds none below its first, and none holds any from its end on: no page of another's is written
+        end = torch.minimum(packed.tensors["end"], pool.tensors["end"])
+        self.ctx.pages_unpack(self.pool_c, self.pool_kr, pool.tensors["table"], cache, pool.tensors["first"], end, batch, self.max_pages, self.stream)
 
     def release(self, rows):
         """The sequences `rows` (an index of any kind) are done: empty from here on, their pages go back with the next fit."""

@@ -1,0 +1,104 @@
+"""GPU tests of PackedSession's rows as requests change hands: a row that is released and taken over by the next call, lengths that fall, pools that have
+no page left.  The contiguous session beside it holds the rows that the pages should hold."""
+import numpy as np
+import pytest
+import torch
+
+import workloads as W
+from paper_2505_13544_amd import binding as B
+from tests.test_gpu_packed_session import check_out, check_state, rows_of, sessions, tokens
+
+pytestmark = pytest.mark.gpu
+
+
+class Served:
+    """Three prompts of 40, 100 and 70 tokens and 45 steps behind them, one token a slot, pages of 16: nine complete pages of sequence 1 were packed, and of
+    the bf16 pages that it gave back for them another sequence holds one (18 pages serve all three)."""
+
+    def __init__(self, n_pages=18, steps=45):
+        self.wl = W.WORKLOADS["speech_bf16"].scaled(name="packed_rows", batch=3, d_model=96, n_heads=8, d_head=64, r=128, d_rope=32, stride=1, prefix=8, steps=4)
+        self.packed, self.flat, self.wts = sessions(self.wl, page_slots=16, max_slots=160, keep=0, n_pages=n_pages)
+        self.make, self.lens = tokens(self.wl, 5), np.array([40, 100, 70], np.int64)
+        self.out = torch.empty(3, 8, 64, dtype=torch.bfloat16, device="cuda")
+        x = self.make(100)
+        n = torch.from_numpy(self.lens.astype(np.int32)).cuda()
+        self.hold = [self.packed.prefill(x["q"], x["q_rope"], x["c"], x["kr"], out=torch.empty(3, 100, 8, 64, device="cuda"), n_new=n)]
+        self.flat.append(x["c"], x["kr"], n_new=n)
+        for _ in range(steps):
+            self.step()
+        self.check("as served")
+
+    def step(self, check=False):
+        x = self.make(1)
+        q, qr = x["q"][:, 0].contiguous(), x["q_rope"][:, 0].contiguous()
+        self.packed.step(x["c"], x["kr"], q, qr, out=self.out)
+        self.flat.append(x["c"], x["kr"])
+        self.lens += 1
+        if check:
+            check_out(self.packed, self.flat, self.wts, self.lens, q, qr, self.out, "a step")
+
+    def prompt(self, row, n, past=0):
+        x = self.make(n)
+        sub = {k: v[row:row + 1].contiguous() for k, v in x.items()}
+        self.hold.append(self.packed.prefill(sub["q"], sub["q_rope"], sub["c"], sub["kr"], out=torch.empty(1, n, 8, 64, device="cuda"), at=row, max_past_slots=past))
+        count = torch.zeros(3, dtype=torch.int32, device="cuda")
+        count[row] = n
+        self.flat.append(x["c"], x["kr"], n_new=count)
+        self.lens[row] += n
+
+    def set_len(self, row, n):
+        self.packed.seq_len[row] = n
+        self.flat.seq_len[row] = n
+        self.lens[row] = n
+
+    def check(self, what):
+        check_state(self.packed, self.flat, self.lens, what)
+
+    def pages(self, b):
+        t = {k: v.cpu().numpy() for k, v in self.packed.pool.tensors.items()}
+        return {int(x) for x in t["table"][b, t["first"][b]:t["end"][b]]}
+
+    def stale(self, b, reach):
+        """Pages that entries of row b from `reach` to the end of its packed ones name, in other sequences' hands."""
+        named = {int(x) for x in self.packed.table[b, reach:int(self.packed.packed.tensors["end"][b])].cpu()}
+        return named & set().union(*(self.pages(i) for i in range(3) if i != b))
+
+
+@pytest.mark.parametrize("n", [20, 7, 150])
+def test_a_released_row_takes_the_next_prompt_at_once(n):
+    # shorter than what was there (also than a page), and longer
+    s = Served()
+    assert s.stale(1, 2), "the case is none: no other sequence holds a page that the row still names"
+    s.packed.release(1)
+    s.flat.seq_len[1] = 0
+    s.lens[1] = 0
+    s.prompt(1, n)
+    s.check("the new prompt")
+    assert int(s.packed.packed.tensors["end"][1]) == n // 16
+    for _ in range(8):                       # across the end of a page of every sequence
+        s.step(check=True)
+    s.check("steps behind it")
+
+
+def test_a_released_row_is_empty_to_unpack():
+    s = Served()
+    s.packed.release(1)
+    s.flat.seq_len[1] = 0
+    s.lens[1] = 0
+    s.packed.unpack(1, 0, at=1)
+    assert not s.pages(1) and int(s.packed.packed.tensors["end"][1]) == 0
+    s.check("unpacked")
+
+
+def test_a_length_that_falls_in_front_of_a_prefill():
+    # the row's pages are unpacked, the length falls to the middle of page 3 of nine that were packed, and a prefill continues there
+    s = Served()
+    lat, _, n4 = rows_of(s.packed, s.flat, 1, int(s.lens[1]))
+    assert n4 == 9
+    s.packed.unpack(1, 0, at=1)
+    s.flat.cache_c[1, :len(lat)] = torch.from_numpy(lat).cuda().bfloat16()      # (rounded as they were packed)
+    s.set_len(1, 50)
+    s.prompt(1, 20, past=50)
+    assert int(s.packed.packed.tensors["end"][1]) == 4
+    s.check("continued")
+    s.step(check=True)
