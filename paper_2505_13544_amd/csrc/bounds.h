@@ -10,9 +10,13 @@ namespace mtla {
   return n < max_slots ? n : max_slots;
 }
 
+// A page count or a page's place in its table row, as the nearest that the row has or ends with.  (Also in front of any sum: max_pages and a
+// launch's pages together stay far from what an int holds, a caller's word does not.)
+[[gnu::always_inline]] constexpr int pages_inside(int page, int max_pages) { return page < 0 ? 0 : (page < max_pages ? page : max_pages); }
+
 // Slots of a sequence that lie in packed pages: `n_packed` pages of 2^shift slots, taken as [0, max_pages].
 [[gnu::always_inline]] constexpr int packed_slots(int n_packed, int max_pages, int shift, int live) {
-  const long long end = (long long)(n_packed < 0 ? 0 : (n_packed < max_pages ? n_packed : max_pages)) << shift;
+  const long long end = (long long)pages_inside(n_packed, max_pages) << shift;
   return end < live ? (int)end : live;
 }
 // Whether they end inside a chunk: what the chunk holds behind them is a piece of its own then, behind those of the chunks.

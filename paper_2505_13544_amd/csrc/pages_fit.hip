@@ -129,12 +129,11 @@ struct Needs {
   int reach, complete;  // end of the entries that its tokens reach, of those that complete pages have
 };
 __device__ __forceinline__ Needs needs_of(const FitArgs& a, const Held& h, bool in) {
-  auto inside = [&](int v) { return v < 0 ? 0 : (v < a.max_pages ? v : a.max_pages); };
   Needs s;
-  s.f = inside(h.f);
-  s.e = inside(h.e);
-  s.f4 = inside(h.f4);
-  s.e4 = inside(h.e4);
+  s.f = pages_inside(h.f, a.max_pages);
+  s.e = pages_inside(h.e, a.max_pages);
+  s.f4 = pages_inside(h.f4, a.max_pages);
+  s.e4 = pages_inside(h.e4, a.max_pages);
   s.n = new_rows(h.n, a.n_new_max);
   // tokens before and after; a length outside 0 .. max_slots * stride counts as the nearer end
   const long long room = (long long)a.max_slots * a.stride;

@@ -6,6 +6,7 @@
 // same in the other direction and exact.  Nothing but bytes bounds either: 2 (r + d_R) bytes of a slot on one side, r / 2 + r / 32 + 2 d_R on the other.
 // At r = 512, d_R = 64: 245500 slots, 283 MB on one side and 98 MB on the other, into packed pages 103 us (3.7 TB/s, where a large sum reads 4.0) and back 64 us (packed
 // pages just written are still in the last-level cache); 500 slots of 16 sequences at r = 256 3.0 and 2.7 us, launches.
+#include "bounds.h"
 #include "mtla_device.h"
 #include "packed.h"
 
@@ -39,14 +40,6 @@ __device__ __forceinline__ PackTile pack_tile(const PackArgs& a, int b, int page
                   a.pk.codes + pt * packed_code_bytes(a.r), a.pk.scales + pt * packed_scale_bytes(a.r), a.pk.keys + pt * (packed_key_bytes(a.d_rope) / 2)};
 }
 
-// Pages of the call: [first, end), inside the table's row.
-__device__ __forceinline__ void page_range(const PackArgs& a, int b, int& first, int& end) {
-  first = a.first ? a.first[b] : 0;
-  end = a.end[b];
-  first = first < 0 ? 0 : first;
-  end = end < a.pages.max_pages ? end : a.pages.max_pages;
-}
-
 // grid = (pages_each * tiles of a page, batch): further pages of a sequence are taken in turns
 template <bool PACK, int R>
 __global__ __launch_bounds__(kBlock) void pack_kernel(PackArgs a) {
@@ -54,8 +47,7 @@ __global__ __launch_bounds__(kBlock) void pack_kernel(PackArgs a) {
   __shared__ __attribute__((aligned(16))) unsigned char s_scales[R / 2];
   const int tid = threadIdx.x, b = blockIdx.y;
   const int tiles_log = a.pages.shift - 4, tile = blockIdx.x & ((1 << tiles_log) - 1);
-  int first, end;
-  page_range(a, b, first, end);
+  const int first = pages_inside(a.first ? a.first[b] : 0, a.pages.max_pages), end = pages_inside(a.end[b], a.pages.max_pages);
   constexpr int RP = R / 8, kPieces = kPackTile * RP;         // 16-byte pieces of a row and of the tile
   constexpr int kOwn = (kPieces + kBlock - 1) / kBlock;       // of a thread: all of them asked for at once
   const int kp = a.d_rope / 8, n_keys = kPackTile * kp;
