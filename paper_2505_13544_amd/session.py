@@ -422,6 +422,16 @@ class PagedSession:
         return self.ctx.device_status(self.workspace, self.stream)
 
 
+def _free_pages(order, n_pages: int) -> np.ndarray:
+    """The pages of a pool in the order that they will be handed out; an `order` may leave some out."""
+    if order is None:
+        return np.arange(n_pages, dtype=np.int32)
+    order = np.asarray(order)
+    if order.ndim != 1 or order.dtype.kind not in "iu" or (order.size and not 0 <= order.min() <= order.max() < n_pages) or len(np.unique(order)) != order.size:
+        raise ValueError(f"page_order: pages of 0 to {n_pages - 1}, none of them twice")
+    return np.ascontiguousarray(order, dtype=np.int32)
+
+
 class PackedSession:
     """Session over paged slot storage whose complete pages are held in 4 bits, with the page tables kept on the device: no call needs
     the lengths on the host, so whole steps, pages changing hands among them, can be captured into a graph and replayed.
@@ -429,7 +439,8 @@ class PackedSession:
     A step is fit (tables follow the lengths), pack (pages completed since go into packed pages, their bf16 pages go back to the pool) and the
     decode step over both kinds of page.  `n_pages` bounds the bf16 pages (per sequence: the ones being written to, the newest `keep_pages` complete
     ones, and one that is between two steps; whole prompts while their prefill runs), `n_packed_pages` the packed ones.  One more bf16 page than
-    that is allocated: what a sequence without a page appends goes there (device_status() then says MTLA_ERR_CAPACITY, refused() how many)."""
+    that is allocated: what a sequence without a page appends goes there (device_status() then says MTLA_ERR_CAPACITY, refused() how many).
+    `page_order`: the bf16 pages in the order that they are handed out (pages that it leaves out are not)."""
 
     def __init__(self, *, n_heads, d_head, r, d_rope, d_hyper, stride, max_batch, max_slots, page_slots, n_pages, n_packed_pages,
                  keep_pages: int = 0, softmax_scale: float = 0.0, device="cuda:0", decode_chunk: Optional[int] = None, page_order=None):
@@ -455,17 +466,16 @@ class PackedSession:
         assert self.codes.numel() == self.ctx.packed_codes_bytes(n_packed_pages)
         assert self.scales.numel() == self.ctx.packed_scales_bytes(n_packed_pages)
         assert self.keys.numel() * 2 == self.ctx.packed_keys_bytes(n_packed_pages)
-        order = torch.arange(n_pages) if page_order is None else torch.as_tensor(np.ascontiguousarray(page_order))
-        order4 = torch.arange(n_packed_pages)
 
-        def pool(ring, spill):
-            return B.PagePool(ints(max_batch, self.max_pages), ints(max_batch), ints(max_batch), ring.to(torch.int32).to(dev),
-                              torch.tensor([0, ring.numel(), 0, 0], dtype=torch.int32, device=dev), was_end=ints(max_batch), spill=spill)
+        def pool(pages, places, spill):
+            ring = ints(places)
+            ring[:len(pages)] = torch.from_numpy(pages).to(dev)
+            return B.PagePool(ints(max_batch, self.max_pages), ints(max_batch), ints(max_batch), ring,
+                              torch.tensor([0, len(pages), 0, 0], dtype=torch.int32, device=dev), was_end=ints(max_batch), spill=spill)
 
         # (the ring of the bf16 pool has a place for every page of the pool, the spill page is in none of them)
-        self.pool = pool(torch.cat([order, torch.full((1,), n_pages)]), n_pages)
-        self.pool.tensors["state"][1] = n_pages
-        self.packed = pool(order4, -1)
+        self.pool = pool(_free_pages(page_order, n_pages), n_pages + 1, n_pages)
+        self.packed = pool(_free_pages(None, n_packed_pages), n_packed_pages, -1)
         self.table = self.pool.tensors["table"]
         self.cache = B.PackedCache(self.codes, self.scales, self.keys, self.packed.tensors["table"], self.packed.tensors["end"])
         self.tail_c = torch.zeros(max_batch, r, dtype=torch.float32, device=dev)

@@ -6,6 +6,7 @@ import torch
 
 import workloads as W
 from paper_2505_13544_amd import binding as B
+from paper_2505_13544_amd.session import PackedSession
 from tests.test_gpu_packed_session import check_out, check_state, rows_of, sessions, tokens
 
 pytestmark = pytest.mark.gpu
@@ -102,3 +103,27 @@ def test_a_length_that_falls_in_front_of_a_prefill():
     assert int(s.packed.packed.tensors["end"][1]) == 4
     s.check("continued")
     s.step(check=True)
+
+
+@pytest.mark.parametrize("as_tensor", [False, True])
+def test_an_order_that_leaves_pages_out(as_tensor):
+    # pages 3, 1 and 5 of eight, in this order, and no other: neither the ones left out nor the page that refused appends go to
+    order = torch.tensor([3, 1, 5]) if as_tensor else [3, 1, 5]
+    s = PackedSession(n_heads=8, d_head=64, r=128, d_rope=32, d_hyper=64, stride=1, max_batch=4, max_slots=48, page_slots=16, n_pages=8, n_packed_pages=4,
+                      page_order=order)
+    s.fit(4, 1, counts=torch.tensor([0, 1, 1, 0], dtype=torch.int32, device="cuda"))
+    assert s.device_status() == B.MTLA_OK and s.table[1, 0] == 3 and s.table[2, 0] == 1
+    s.fit(4, 1)
+    assert s.refused() == (1, 0) and s.device_status() == B.MTLA_ERR_CAPACITY
+    t = s.pool.tensors
+    assert s.table[0, 0] == 5 and t["end"].tolist() == [1, 1, 1, 0] and s.table[3, 0] == 8       # (the page behind the pool's eight)
+    s.fit(4)
+    assert s.device_status() == B.MTLA_OK and int(t["state"][1]) == 3
+    assert sorted(t["ring"][[(int(t["state"][0]) + i) % 9 for i in range(3)]].tolist()) == [1, 3, 5]
+
+
+@pytest.mark.parametrize("order", [[0, 1, 1], [0, 8], [-1, 2], list(range(9)), [[0, 1]], [0.5, 1.0]])
+def test_orders_that_are_none(order):
+    with pytest.raises((ValueError, TypeError)):
+        PackedSession(n_heads=8, d_head=64, r=128, d_rope=32, d_hyper=64, stride=1, max_batch=4, max_slots=48, page_slots=16, n_pages=8, n_packed_pages=4,
+                      page_order=order)
