@@ -518,8 +518,10 @@ class PackedSession:
         stay as they are; the next fit gives the bf16 ones back."""
         # both pools as the lengths are now: a row released since, or cut short, has packed pages that are not its tokens'
         self.fit(batch, at=at)
+        before = self._refusals()
         pool, packed, cache = self._part(at)
         self.ctx.pages_fit(pool, None, self.seq_len[at:], counts, n_new, 0, batch, slot_map, self.workspace, self.stream)
+        self._refusals(before)
         # a sequence that got no pages holds none below its first, and none holds any from its end on: no page of another's is written
         end = torch.minimum(packed.tensors["end"], pool.tensors["end"])
         self.ctx.pages_unpack(self.pool_c, self.pool_kr, pool.tensors["table"], cache, pool.tensors["first"], end, batch, self.max_pages, self.stream)
@@ -529,8 +531,17 @@ class PackedSession:
         self.seq_len[rows] = 0
 
     def refused(self):
-        """Sequences that the last fit had no page for, in the bf16 pool and in the packed one."""
+        """Sequences that the last call (fit, unpack, prefill, step) had no page for, in the bf16 pool and in the packed one; of a call that fits the tables
+        more than once, the most that one of its fits refused."""
         return int(self.pool.tensors["state"][2]), int(self.packed.tensors["state"][2])
+
+    def _refusals(self, before=None):
+        """The counts as they are on the device; with those of `before`, the larger ones from here on (a fit starts them anew)."""
+        counts = [p.tensors["state"][2] for p in (self.pool, self.packed)]
+        if before is None:
+            return [n.clone() for n in counts]
+        for n, more in zip(counts, before):
+            torch.maximum(n, more, out=n)
 
     # ---- calls
     def prefill(self, q, q_rope, c, kr, *, out, max_past_slots: int = 0, n_new=None, w_out=None, at: int = 0):
@@ -542,7 +553,9 @@ class PackedSession:
         self.ctx.prefill_step_paged(self.pool_c, self.pool_kr, self.tail_c[at:], self.seq_len[at:], self.table[at:], q, q_rope, c, kr, n_new,
                                     self.hyp_A, self.hyp_a, self.hyp_G, self.w_uk, self.w_uv, batch, T, max_past_slots, out, w_out,
                                     scratch, self.workspace, self.stream)
+        before = self._refusals()
         self.fit(batch, at=at)
+        self._refusals(before)
         return scratch  # keep alive until the stream has consumed it
 
     def decode(self, q, q_rope, *, out=None, out_latent=None, lse=None):

@@ -127,3 +127,36 @@ def test_orders_that_are_none(order):
     with pytest.raises((ValueError, TypeError)):
         PackedSession(n_heads=8, d_head=64, r=128, d_rope=32, d_hyper=64, stride=1, max_batch=4, max_slots=48, page_slots=16, n_pages=8, n_packed_pages=4,
                       page_order=order)
+
+
+def test_a_prefill_that_lacked_pages_says_how_many():
+    # six bf16 pages: prompts of 40, 30 and 33 tokens need 3 + 2 + 3, so the third gets none (its tokens go to the page that is nobody's).  The fit behind
+    # the prefill refuses nobody, and must not hide that; no row of the others is harmed
+    wl = W.WORKLOADS["speech_bf16"].scaled(name="packed_refused", batch=3, d_model=96, n_heads=8, d_head=64, r=128, d_rope=32, stride=1, prefix=8, steps=4)
+    packed, flat, _ = sessions(wl, page_slots=16, max_slots=160, keep=0, n_pages=6)
+    make, n = tokens(wl, 3), torch.tensor([40, 30, 33], dtype=torch.int32, device="cuda")
+    x = make(40)
+    hold = packed.prefill(x["q"], x["q_rope"], x["c"], x["kr"], out=torch.empty(3, 40, 8, 64, device="cuda"), n_new=n)
+    flat.append(x["c"], x["kr"], n_new=n)
+    assert packed.refused()[0] == 1 and packed.device_status() == B.MTLA_ERR_CAPACITY
+    packed.release(2)
+    flat.seq_len[2] = 0
+    packed.fit(3)
+    check_state(packed, flat, [40, 30, 0], "the others")          # (refused() == (0, 0) among it)
+    del hold
+
+
+def test_a_prefill_that_found_room_behind_its_packing():
+    # the packed pool holds two pages: the second prompt's do not fit, and stay bf16; nothing is lost, and both pools say what they refused
+    wl = W.WORKLOADS["speech_bf16"].scaled(name="packed_refused", batch=2, d_model=96, n_heads=8, d_head=64, r=128, d_rope=32, stride=1, prefix=8, steps=4)
+    packed, flat, _ = sessions(wl, page_slots=16, max_slots=160, keep=0, n_pages=12, n_packed=2)
+    make, n = tokens(wl, 3), torch.tensor([40, 70], dtype=torch.int32, device="cuda")
+    x = make(70)
+    hold = packed.prefill(x["q"], x["q_rope"], x["c"], x["kr"], out=torch.empty(2, 70, 8, 64, device="cuda"), n_new=n)
+    assert packed.refused() == (0, 1) and packed.device_status() == B.MTLA_ERR_CAPACITY
+    assert packed.packed.tensors["end"].tolist() == [2, 0] and packed.pool.tensors["first"].tolist() == [2, 0]
+    packed.unpack(1, 8, at=1)                                     # alone: what the last call lacked
+    assert packed.refused() == (0, 1) and packed.device_status() == B.MTLA_ERR_CAPACITY
+    packed.unpack(1, 8)
+    assert packed.refused() == (0, 0) and packed.device_status() == B.MTLA_OK
+    del hold
