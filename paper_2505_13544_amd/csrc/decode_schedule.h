@@ -36,6 +36,12 @@ constexpr bool packed_wide(int r, int batch, int n_heads, int chunks, int chunk)
   return r == 512 && groups <= 4 && chunk >= 256 && groups * (chunks + 1LL) <= 256;
 }
 
+// Page tables on the device: sequences that a workgroup takes (a wavefront's lanes, or 16 of them: a quarter of the long intervals to carry, as long as a wavefront
+// reads the groups' sums at once), and the bytes that a call of up to `max_batch` sequences keeps such sums in, 16 a group and 16 for the rings.
+constexpr int fit_group(int batch) { return batch <= 64 || batch > 1024 ? 64 : 16; }
+constexpr int fit_groups(int batch) { return (batch + fit_group(batch) - 1) / fit_group(batch); }
+constexpr long long fit_scratch_bytes(int max_batch) { return 16 * (max_batch / 16 + 2LL); }  // (1024 sequences have more groups than 1025)
+
 // Whether a call of `batch` sequences of up to `max_slots` slots takes the balanced schedule rather than static chunks; `chunk_set`: by the caller.
 // The balanced one has a fixed cost, the scan of the lengths and a cold start of every persistent workgroup, some 5 us of a step beside a
 // chunk a workgroup, and its partials are halves.  Below 8 tiles of 16 slots a unit it is left out: with partials in fp32, as the chunks' are, it would gain there only with

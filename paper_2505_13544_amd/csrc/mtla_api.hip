@@ -76,7 +76,8 @@ DecodeLayout decode_layout(const mtla_ctx* c) {
   DecodeLayout L;
   L.prefix = kHeaderBytes;
   L.qcat = align_up(L.prefix + (B + 1) * 4, 256);
-  L.part_o = align_up(L.qcat + B * nh * E * 4, 256);
+  const size_t query = B * nh * E * 4, sums = (size_t)fit_scratch_bytes(g.max_batch);  // (mtla_pages_fit's sums lie there too)
+  L.part_o = align_up(L.qcat + (query > sums ? query : sums), 256);
   L.part_ml = align_up(L.part_o + P * nh * g.r * 4, 256);
   L.total = align_up(L.part_ml + P * nh * 2 * 4, 256);
   return L;
@@ -679,7 +680,7 @@ inline bool fit_pool(const mtla_page_pool* p, int page_slots, FitPool& out) {
 
 mtla_status mtla_pages_fit(mtla_ctx* c, const mtla_page_pool* pool, const mtla_page_pool* packed, const int32_t* seq_len, const int32_t* n_new,
                            int32_t n_new_max, int32_t keep_pages, int32_t batch, int64_t* slot_map, void* workspace, void* hip_stream) {
-  if (!c || !seq_len || !workspace) return MTLA_ERR_INVALID_ARG;
+  if (!c || !seq_len || !workspace || !aligned16(workspace)) return MTLA_ERR_INVALID_ARG;
   const mtla_config& g = c->cfg;
   if (g.page_slots <= 0 || batch < 1 || batch > g.max_batch || n_new_max < 0 || keep_pages < 0) return MTLA_ERR_INVALID_ARG;
   if (slot_map && (n_new_max < 1 || n_new_max > 1 << 30)) return MTLA_ERR_INVALID_ARG;

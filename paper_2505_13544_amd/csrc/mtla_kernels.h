@@ -354,7 +354,7 @@ struct FitArgs {
   const int32_t* n_new;       // [batch] or NULL: n_new_max
   int64_t* slot_map;          // [batch, n_new_max] or NULL
   int32_t* status;            // workspace header word
-  void* scratch;              // 16-byte aligned: 16 bytes for every 64 sequences and 16 more
+  void* scratch;              // 16-byte aligned, fit_scratch_bytes(batch)
   int n_new_max, keep_pages, batch, max_pages, stride, max_slots, shift;
 };
 

@@ -16,6 +16,7 @@
 //   256 that take 40 pages each       2.3 + 7.3 (groups of 64: 1.9 + 11.5), 13.5
 //   3001, drafts of 8, two pools      3.2 + 7.5, 25.2 + 5.1
 #include "bounds.h"
+#include "decode_schedule.h"
 #include "mtla_device.h"
 #include "packed.h"
 
@@ -165,6 +166,7 @@ __device__ __forceinline__ void put_ring(const FitPool& p, const Ring& r, int ta
 struct Sums {
   int take4, take, give, give4;
 };
+static_assert(sizeof(Sums) == 16, "fit_scratch_bytes");
 constexpr int kSumCap = 1 << 29;  // (more than any pool has pages)
 
 // sums[i] of the i-th `group` (16 or 64) sequences, and behind them the rings
@@ -435,8 +437,7 @@ __global__ __launch_bounds__(kBlock) void slot_map_kernel(FitArgs a) {
 
 hipError_t launch_pages_fit(const FitArgs& a, hipStream_t st) {
   const bool own_map = a.slot_map && a.n_new_max <= kOwnTokens;
-  // groups of 16 (a quarter of the long intervals to carry) as long as a wavefront reads their sums at once
-  const int group = a.batch <= kWave || a.batch > 1024 ? kWave : 16, n = (a.batch + group - 1) / group;
+  const int group = fit_group(a.batch), n = fit_groups(a.batch);
   Sums* sums = n > 1 ? reinterpret_cast<Sums*>(a.scratch) : nullptr;
   if (sums) {
     hipLaunchKernelGGL(pages_sums_kernel, dim3((a.batch + kBlock - 1) / kBlock), dim3(kBlock), 0, st, a, sums, n, group);

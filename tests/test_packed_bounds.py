@@ -1,9 +1,13 @@
-"""Which pages the packing kernels walk, compiled and run on the host: their own bounds and their own loop, for words in the arrays that hold anything."""
+"""Bounds of the calls for packed pages, on the host: which pages the packing kernels walk (their own bounds and their own loop, for words in the arrays that
+hold anything), and the sums that the page tables' launches keep in the workspace."""
 import os
 import shutil
 import subprocess
 
 import pytest
+import torch
+
+from paper_2505_13544_amd import binding as B
 
 CSRC = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "paper_2505_13544_amd", "csrc")
 
@@ -49,3 +53,34 @@ def test_the_kernel_bounds_both_ends():
     src = open(os.path.join(CSRC, "pages_pack.hip")).read()
     assert src.count("a.first[b]") == src.count("pages_inside(a.first ? a.first[b] : 0, a.pages.max_pages)") == 1
     assert src.count("a.end[b]") == src.count("pages_inside(a.end[b], a.pages.max_pages)") == 1
+
+
+SUMS = r"""
+#include "decode_schedule.h"
+#include <initializer_list>
+using namespace mtla;
+int main() {
+  for (int most = 1; most <= 65535; ++most) {
+    const long long room = fit_scratch_bytes(most);
+    if (room > most * 96LL * 4) return 1;   // a context's smallest query: one head, r = 64 and 32 RoPE columns
+    for (int batch : {1, 64, 65, 1023, 1024, 1025, most - 1, most})
+      if (batch >= 1 && batch <= most && (fit_groups(batch) * fit_group(batch) < batch || 16LL * (fit_groups(batch) + 1) > room)) return 2;
+  }
+  return 0;
+}
+"""
+
+
+@pytest.mark.skipif(not shutil.which("g++"), reason="no host compiler")
+def test_the_sums_of_the_page_tables_fit_where_they_lie(tmp_path):
+    (tmp_path / "main.cpp").write_text(SUMS)
+    subprocess.run(["g++", "-std=c++17", "-Wall", "-Werror", "-I", CSRC, str(tmp_path / "main.cpp"), "-o", str(tmp_path / "main")], check=True)
+    subprocess.run([str(tmp_path / "main")], check=True)
+
+
+def test_page_tables_refuse_a_workspace_that_is_not_aligned():
+    ctx = B.Context(n_heads=8, d_head=64, r=256, d_rope=32, d_hyper=64, stride=2, max_batch=16, max_slots=640, dtype="bf16", page_slots=64, n_pages=40)
+    ints = lambda *s: torch.zeros(*s, dtype=torch.int32)
+    pool = B.PagePool(ints(16, 10), ints(16), ints(16), ints(40), ints(4))
+    for workspace in (1028, 1032, 1025):
+        assert ctx.pages_fit_status(pool, None, 1024, None, 1, 0, 16, None, workspace) == B.MTLA_ERR_INVALID_ARG
