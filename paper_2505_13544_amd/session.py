@@ -491,12 +491,17 @@ class PackedSession:
     set_weights = Session.set_weights
 
     # ---- pages
-    def _part(self, at: int):
-        """Tables and state of the sequences from `at` on: (pool, packed pool, packed cache)."""
-        if at == 0:
+    def _part(self, at: int, batch: int, n_new: int, counts, slot_map):
+        """Tables and state of the sequences from `at` on: (pool, packed pool, packed cache), for a call of `batch` of them with these arrays."""
+        for name, t, dtype, n in (("counts", counts, "int32", batch), ("slot_map", slot_map, "int64", batch * n_new)):
+            if t is not None:
+                B._device_array(name, t, dtype)
+                if t.numel() < n:
+                    raise ValueError(f"{name}: {n} entries are needed for {batch} sequences and {n_new} tokens")
+        if at == 0:  # (the library refuses a batch that the context lacks)
             return self.pool, self.packed, self.cache
-        if not 0 < at < self.max_batch:
-            raise IndexError(f"sequence {at} of a session of {self.max_batch}")
+        if not 0 < at < self.max_batch or at + batch > self.max_batch:
+            raise IndexError(f"sequences {at} to {at + batch - 1} of a session of {self.max_batch}")
 
         def part(p):
             t = p.tensors
@@ -508,7 +513,7 @@ class PackedSession:
     def fit(self, batch: int, n_new: int = 0, *, counts=None, slot_map=None, at: int = 0):
         """Tables of sequences at .. at + batch - 1 for n_new more tokens (counts: an int32 device tensor of how many of them, per
         sequence); pages completed since the last call are packed."""
-        pool, packed, cache = self._part(at)
+        pool, packed, cache = self._part(at, batch, n_new, counts, slot_map)
         self.ctx.pages_fit(pool, packed, self.seq_len[at:], counts, n_new, self.keep_pages, batch, slot_map, self.workspace, self.stream)
         t = packed.tensors
         self.ctx.pages_pack(self.pool_c, self.pool_kr, pool.tensors["table"], cache, t["was_end"], t["end"], batch, 1, self.stream)
@@ -516,10 +521,10 @@ class PackedSession:
     def unpack(self, batch: int, n_new: int = 0, *, counts=None, slot_map=None, at: int = 0):
         """The sequences in bf16 pages alone, with room for n_new more tokens: what a prefill that continues them reads.  Their packed pages
         stay as they are; the next fit gives the bf16 ones back."""
+        pool, packed, cache = self._part(at, batch, n_new, counts, slot_map)
         # both pools as the lengths are now: a row released since, or cut short, has packed pages that are not its tokens'
         self.fit(batch, at=at)
         before = self._refusals()
-        pool, packed, cache = self._part(at)
         self.ctx.pages_fit(pool, None, self.seq_len[at:], counts, n_new, 0, batch, slot_map, self.workspace, self.stream)
         self._refusals(before)
         # a sequence that got no pages holds none below its first, and none holds any from its end on: no page of another's is written

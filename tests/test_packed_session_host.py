@@ -15,3 +15,34 @@ def test_free_pages():
     for order in ([0, 1, 1], [0, 5], [-1, 2], [[0, 1]], [0.0, 1.0], list(range(6)), [True, False], 3):
         with pytest.raises(ValueError):
             S._free_pages(order, 5)
+
+
+def session(max_batch):
+    s = object.__new__(S.PackedSession)
+    s.max_batch = max_batch
+    return s
+
+
+@pytest.mark.parametrize("batch,at", [(3, 1), (1, 3), (2, 2), (1, -1), (1 << 20, 1), (1, 1 << 20)])
+def test_sequences_that_a_session_lacks(batch, at):
+    # refused before a call is made (there is no GPU, and nothing else of a session, here)
+    s = session(3)
+    with pytest.raises(IndexError):
+        s.fit(batch, at=at)
+    with pytest.raises(IndexError):
+        s.unpack(batch, 4, at=at)
+    x = torch.zeros(batch if batch < 9 else 9, 5, 64)
+    with pytest.raises(IndexError):
+        s.prefill(x, x, x, x, out=None, at=at)
+
+
+@pytest.mark.parametrize("call", ["fit", "unpack"])
+def test_arrays_that_are_none_of_the_call(call):
+    s = session(3)
+    ints, longs = lambda *n: torch.zeros(*n, dtype=torch.int32), lambda *n: torch.zeros(*n, dtype=torch.int64)
+    for kw in (dict(counts=longs(3)), dict(counts=[1, 2, 3]), dict(counts=ints(6)[::2]), dict(slot_map=ints(3, 4)), dict(slot_map=longs(4, 3).t())):
+        with pytest.raises(TypeError):
+            getattr(s, call)(3, 4, **kw)
+    for kw in (dict(counts=ints(2)), dict(slot_map=longs(3, 3)), dict(slot_map=longs(11))):
+        with pytest.raises(ValueError):
+            getattr(s, call)(3, 4, **kw)
