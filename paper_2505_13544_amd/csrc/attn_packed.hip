@@ -670,7 +670,7 @@ __device__ __forceinline__ void stream_open(Worker<C>& w, const Source& s, Chunk
   }
 }
 
-struct Run {  // slots [k0, k1) of sequence b, k0 < k1, k0 a multiple of 16
+struct Run {  // slots [k0, k1) of sequence b, k0 < k1, k0 a multiple of 16: all of them packed, or none
   int b, k0, k1, piece;
   int packed;  // the sequence's slots that lie in packed pages
 };
@@ -716,15 +716,14 @@ __device__ __forceinline__ void attend_run(const AttnPackedArgs& a, const Run& r
   const int k0 = run.k0, k1 = run.k1, tid = threadIdx.x, wv = m.wv;
   const QueryRope<C>& qr = head.qr;
   Worker<C> w(m, smem);
-  const int kp = run.packed < k1 ? run.packed : k1;  // slots below it come out of packed pages
-  const int ko = kp > k0 ? kp : k0;
   ChunkPages pages = chunk_pages(head.entries, s, k0 >> s.shift, m.lane);
-  if (kp > k0) stream_packed<C>(w, s, pages, head.q, qr, k0, kp);
-  if (k1 > ko) {
+  if (run.packed > k0) {
+    stream_packed<C>(w, s, pages, head.q, qr, k0, k1);
+  } else {
     OpenStep<C> o;
     o.q.load(query_rows<C>(at, run.b, h0), at.q_plane, heads, m);
-    load_open<C, 0, C::TL>(o, s, pages, ko, k1, m);
-    stream_open<C>(w, s, pages, o, qr, ko, k1);
+    load_open<C, 0, C::TL>(o, s, pages, k0, k1, m);
+    stream_open<C>(w, s, pages, o, qr, k0, k1);
   }
 
   // ---- normalisers and references of the groups
