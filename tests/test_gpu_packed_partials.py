@@ -6,7 +6,7 @@ import numpy as np
 import pytest
 import torch
 
-from tests.test_gpu_packed import Case
+from tests.test_gpu_packed import Case, context
 
 pytestmark = pytest.mark.gpu
 
@@ -56,3 +56,13 @@ def test_latents_of_any_size(n_heads, d_head, r, slots, packed, chunk, power):
     no, nol, nls = c.run()
     assert np.array_equal(nls, ls)
     assert np.array_equal(nol, np.ldexp(ol, power)) and np.array_equal(no, np.ldexp(o, power))
+
+
+@pytest.mark.parametrize("n_heads,r,max_batch,max_slots", [(16, 512, 256, 8192), (8, 256, 512, 2048), (20, 128, 64, 32768), (8, 64, 1, 60000), (16, 512, 3, 60000)])
+def test_few_short_sequences_in_a_large_context(n_heads, r, max_batch, max_slots):
+    # the chunk follows the context's sequences, the call's are fewer and shorter: long chunks of which one is in use, and a join of many pieces that are not there
+    slots = [700, 33, 0, 1500][:max_batch]
+    c = Case(n_heads=n_heads, d_head=64, r=r, d_rope=32, stride=1, page_slots=64, lens=slots, packed=[10, 0, 0, 23][:max_batch], max_slots=max_slots, seed=r)
+    c.ctx, c.ws = context(n_heads=n_heads, d_head=64, r=r, d_rope=32, stride=1, max_batch=max_batch, max_slots=max_slots, page_slots=64,
+                          n_pages=c.cache_c.shape[0])
+    c.check()

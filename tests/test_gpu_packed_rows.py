@@ -7,6 +7,7 @@ import torch
 import workloads as W
 from paper_2505_13544_amd import binding as B
 from paper_2505_13544_amd.session import PackedSession
+from tests import packed_reference as P
 from tests.test_gpu_packed_session import check_out, check_state, rows_of, sessions, tokens
 
 pytestmark = pytest.mark.gpu
@@ -159,4 +160,52 @@ def test_a_prefill_that_found_room_behind_its_packing():
     assert packed.refused() == (0, 1) and packed.device_status() == B.MTLA_ERR_CAPACITY
     packed.unpack(1, 8)
     assert packed.refused() == (0, 0) and packed.device_status() == B.MTLA_OK
+    del hold
+
+
+@pytest.mark.parametrize("n_pages,n_packed", [(3, 9), (4, 3), (3, 3), (6, 9)])
+def test_pools_that_run_out_while_serving(n_pages, n_packed):
+    # rows of 20, 10 and no tokens go on by 40: what the rules by plain loops refuse, step by step, in either pool.  A token of a row without a page lies in the
+    # page that is nobody's; rows that never lacked one stay what they should be
+    wl = W.WORKLOADS["speech_bf16"].scaled(name="packed_out", batch=3, d_model=96, n_heads=8, d_head=64, r=128, d_rope=32, stride=1, prefix=8, steps=4)
+    packed, flat, _ = sessions(wl, page_slots=16, max_slots=96, keep=0, n_pages=n_pages, n_packed=n_packed)
+    make, n = tokens(wl, 11), torch.tensor([20, 10, 0], dtype=torch.int32, device="cuda")
+    x = make(20)
+    hold = packed.prefill(x["q"], x["q_rope"], x["c"], x["kr"], out=torch.empty(3, 20, 8, 64, device="cuda"), n_new=n)
+    flat.append(x["c"], x["kr"], n_new=n)
+    ref = P.Pool(3, 6, np.random.default_rng(0).permutation(n_pages), n_pages + 1, n_pages)
+    ref4 = P.Pool(3, 6, np.arange(n_packed))
+    fit = lambda lens, new, four=ref4, most=1: P.fit(ref, four, lens, new, page_slots=16, stride=1, max_slots=96, keep=0, batch=3, n_max=most)
+    fit([0] * 3, [0] * 3), fit([0] * 3, [20, 10, 0], None, 20), fit([20, 10, 0], [0] * 3)
+    lens, out = np.array([20, 10, 0]), torch.empty(3, 8, 64, dtype=torch.bfloat16, device="cuda")
+    lost, spilled, refused4 = set(), 0, 0
+    assert packed.device_status() == B.MTLA_OK
+    for t in range(40):
+        x = make(1)
+        packed.step(x["c"], x["kr"], x["q"][:, 0].contiguous(), x["q_rope"][:, 0].contiguous(), out=out)
+        flat.append(x["c"], x["kr"])
+        rows = fit(lens, [1] * 3)
+        assert packed.refused() == (ref.refused, ref4.refused), t
+        assert packed.device_status() == (B.MTLA_ERR_CAPACITY if ref.refused or ref4.refused else B.MTLA_OK), t
+        refused4 += ref4.refused
+        where = {}
+        for b in range(3):
+            if rows[b, 0] < 0:                      # its token has no page
+                assert int(packed.table[b, lens[b] // 16]) == n_pages
+                where.setdefault(int(lens[b]) % 16, []).append(b)
+                lost.add(b)
+                spilled += 1
+        for slot, who in where.items():             # (of two tokens of one slot either one)
+            assert any(torch.equal(packed.pool_c[n_pages, slot], flat.cache_c[b, lens[b]]) for b in who), t
+        lens += 1
+        for b in set(range(3)) - lost:
+            lat, _, n4 = rows_of(packed, flat, b, int(lens[b]))
+            assert n4 == int(ref4.end[b])
+            t16, t4 = packed.table[b].long(), packed.packed.tensors["table"][b].long()
+            got = packed.pool_c[t16[n4:-(-int(lens[b]) // 16)]].reshape(-1, 128)[:int(lens[b]) - 16 * n4].double().cpu().numpy()
+            assert np.array_equal(got, lat[16 * n4:]), (t, b)
+            if n4:
+                c, _ = P.page_rows(packed.codes[t4[:n4]].cpu().numpy(), packed.scales[t4[:n4]].cpu().numpy(), packed.keys[t4[:n4]].double().cpu().numpy())
+                assert np.array_equal(c.reshape(-1, 128), lat[:16 * n4]), (t, b)
+    assert (spilled > 0) == (n_pages < 6) and (refused4 > 0) == (n_packed < 9)
     del hold
