@@ -19,8 +19,8 @@
 // to 6 x 2^125, and a half, for all that it is half the bytes to join, holds 11 bits of numbers from 2^-14 to 65504.
 //
 // Between two barriers a wavefront forms the values of step i - 1, the weights of step i and the logits of step i + 1.  What bounds it, r = 512, 16 heads:
-//   512 x 1024 slots (two workgroups a unit)  52 us, 4.0 TB/s: half the time VALU, a quarter MFMA, and the memory (47 us with all pages in L2)
-//   256 x 1024 slots, chunks of 512           33 us, 3.2 TB/s: a step of 64 slots is 1.7 us alone on a unit, 2.4 beside another workgroup's
+//   512 x 1024 slots (two workgroups a unit)  54 us, 3.8 TB/s: half the time VALU, a quarter MFMA, and the memory (50 us with all pages in L2)
+//   256 x 1024 slots, chunks of 512           34 us, 3.0 TB/s: a step of 64 slots is 1.7 us alone on a unit, 2.4 beside another workgroup's
 //   256 x 32 slots                            9 us: the launch, two reads that wait for each other (0.7 us each, 1.6 with all units reading), an open step (2.3)
 // Tried and left: an equal share of all steps for each of 512 workgroups (ahead of the above 47 us instead of 49 where 256 lengths range from 256 to 2048 slots, but 37
 // instead of 32 where all are 1024: its scan of the lengths is one more read to wait for); the open page in front of the packed ones, its rows asked for early (no gain).

@@ -13,15 +13,15 @@ constexpr int decode_chunk(int max_batch, int max_slots) {
 
 // The same over packed pages, whose kernel gives every 16 heads workgroups of their own; and no more than 256 chunks of a sequence, which one workgroup a head
 // joins.  us of attention + join at r = 512, chunks of 128 / 256 / 512 / 1024 slots:
-//   8 x 8192, 32 heads            24.7 + 9.2 / 19.8 + 7.2 / 20.6 + 7.0 / 30.2 + 6.8
-//   256 x 256 to 2048, 16 heads   78.0 + 14.6 / 59.5 + 11.6 / 49.8 + 10.0 / 45.4 + 9.0
-//   1 x 131071, 16 heads          25.4 + 38.1 / 23.8 + 21.9 / 23.6 + 14.1 (four wavefronts)
+//   8 x 8192, 32 heads            26.5 + 10.8 / 20.9 + 8.2 / 20.9 + 7.0 / 30.0 + 6.8
+//   256 x 256 to 2048, 16 heads   85 + 20 / 63.6 + 14.6 / 51.7 + 11.9 / 46.0 + 10.4
+//   1 x 131071, 16 heads          30.2 + 36.8 / 23.7 + 20.6 / 23.6 + 13.5 (four wavefronts)
 // At r = 512 up to four of these groups of heads and sequences take workgroups of eight wavefronts (packed_wide), one a unit, in chunks that leave room for the
 // pieces behind the packed slots: as many steps side by side on a unit as two workgroups of four, and half of the pieces.  us, attention + join, wide / the best
 // of four wavefronts:
-//   16 heads   1 x 131071 22.6 + 12.5 / 23.6 + 14.1, 1 x 65536 (chunks of 512) 17.9 + 9.3 / 15.8 + 13.8, 2 x 131071 32.0 + 10.1 / 36.3 + 10.2,
-//              4 x 131071 52.0 + 8.8 / 57.3 + 10.5, 4 x 32768 21.8 + 7.6 / 22.5 + 8.4
-//   32 heads   1 x 131071 30.3 + 9.8 / 35.6 + 10.2, but 8 x 8192 19.8 + 6.8 / 18.9 + 6.9
+//   16 heads   1 x 131071 21.5 + 12.1 / 23.6 + 13.5, 1 x 65536 (chunks of 512) 18.0 + 9.4 / 16.6 + 13.5, 2 x 131071 31.9 + 9.5 / 31.5 + 12.5,
+//              4 x 131071 52.0 + 8.4 / 59.2 + 10.6, 4 x 32768 21.6 + 7.6 / 23.0 + 8.2
+//   32 heads   1 x 131071 30.8 + 9.5 / 30.2 + 12.8, but 8 x 8192 (chunks of 576) 21.4 + 7.2 / 20.9 + 7.0
 constexpr int packed_chunk(int r, int max_batch, int max_slots, int n_heads) {
   const int groups = max_batch * ((n_heads + 15) / 16);
   if (r == 512 && groups <= 4) {
