@@ -816,7 +816,7 @@ __global__ __launch_bounds__(W * kWave, 2) void attn_packed_kernel(AttnPackedArg
   if (behind) {
     const int chunk_end = at.chunk - run.packed % at.chunk;  // (slots from k0 on)
     run.k1 = live - run.k0 < chunk_end ? live : run.k0 + chunk_end;
-    run.piece = run.b * at.n_splits + (live + at.chunk - 1) / at.chunk;
+    run.piece = run.b * at.n_splits + chunks_of(live, at.chunk);
   } else {
     live = live_slots(len, at.stride, at.max_slots);
     if (run.k0 >= live) return;

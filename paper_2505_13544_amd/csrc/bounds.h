@@ -10,6 +10,9 @@ namespace mtla {
   return n < max_slots ? n : max_slots;
 }
 
+// Chunks that `live` slots have, for any two ints (a caller's chunk may be the largest multiple of 32).
+[[gnu::always_inline]] constexpr int chunks_of(int live, int chunk) { return live / chunk + (live % chunk != 0 ? 1 : 0); }
+
 // A page count or a page's place in its table row, as the nearest that the row has or ends with.  (Also in front of any sum: max_pages and a
 // launch's pages together stay far from what an int holds, a caller's word does not.)
 [[gnu::always_inline]] constexpr int pages_inside(int page, int max_pages) { return page < 0 ? 0 : (page < max_pages ? page : max_pages); }

@@ -68,7 +68,7 @@ __device__ __forceinline__ Pieces pieces_of_row(const CombineArgs& a, int row, i
       live = m < len ? m / a.stride + 1 : 0;
     }
     p.first = row * a.n_splits;
-    p.count = (live + a.chunk - 1) / a.chunk;
+    p.count = chunks_of(live, a.chunk);
     if (a.n_packed && open_piece(packed_slots(a.n_packed[row], a.max_pages, a.shift, live), live, a.chunk)) ++p.count;
   }
   return p;

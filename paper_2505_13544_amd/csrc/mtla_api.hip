@@ -10,6 +10,7 @@
 #include <new>
 #include <vector>
 
+#include "bounds.h"
 #include "decode_schedule.h"
 #include "mtla_device.h"
 #include "mtla_kernels.h"
@@ -37,7 +38,7 @@ using namespace mtla;
 inline size_t align_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
 inline size_t elem_size(int dtype) { return dtype == MTLA_F32 ? 4 : 2; }
 
-inline int n_splits(const mtla_ctx* c) { return (c->cfg.max_slots + c->chunk - 1) / c->chunk; }
+inline int n_splits(const mtla_ctx* c) { return chunks_of(c->cfg.max_slots, c->chunk); }
 
 // Persistent workgroups of the balanced decode schedule: one per compute unit, at most this many.
 constexpr int kMaxPersistent = 1024;
@@ -50,7 +51,7 @@ constexpr int kBalancedMaxBatch = 2048;  // the running tile counts of a batch l
 
 // Slots of a chunk over packed pages, and a sequence's pieces: the chunks, and one for what lies behind the packed slots in theirs.
 inline int packed_chunk(const mtla_ctx* c) { return c->chunk_set ? c->chunk : mtla::packed_chunk(c->cfg.r, c->cfg.max_batch, c->cfg.max_slots, c->cfg.n_heads); }
-inline int packed_splits(const mtla_ctx* c) { return (c->cfg.max_slots + packed_chunk(c) - 1) / packed_chunk(c) + 1; }
+inline int packed_splits(const mtla_ctx* c) { return chunks_of(c->cfg.max_slots, packed_chunk(c)) + 1; }
 
 // Partials ("pieces") the decode pass can emit: chunks x sequences under the static schedule,
 // one per persistent workgroup plus one per sequence under the balanced one.

@@ -178,7 +178,7 @@ __global__ __launch_bounds__(kBlock) void combine_kernel(CombineArgs a) {
     n_avail = a.n_splits;
     const int live = a.T == 0 ? live_slots(len, a.stride, a.max_slots) : (mrow < len ? mrow / a.stride + 1 : 0);
     empty = live == 0;
-    nsp = (live + a.chunk - 1) / a.chunk;
+    nsp = chunks_of(live, a.chunk);
     if (a.n_packed && open_piece(packed_slots(a.n_packed[row], a.max_pages, a.shift, live), live, a.chunk)) ++nsp;
   }
   const size_t pb = (size_t)piece0 * a.n_heads + h;  // + sp * n_heads

@@ -66,3 +66,14 @@ def test_few_short_sequences_in_a_large_context(n_heads, r, max_batch, max_slots
     c.ctx, c.ws = context(n_heads=n_heads, d_head=64, r=r, d_rope=32, stride=1, max_batch=max_batch, max_slots=max_slots, page_slots=64,
                           n_pages=c.cache_c.shape[0])
     c.check()
+
+
+@pytest.mark.parametrize("n_heads,r", [(8, 64), (16, 256), (20, 512), (16, 512)])
+def test_a_chunk_that_holds_every_slot(n_heads, r):
+    # the largest chunk that can be set is one chunk, and whole sequences in one chunk are the same whatever its size
+    c = Case(n_heads=n_heads, d_head=64, r=r, d_rope=32, stride=1, page_slots=16, lens=[300, 33, 0, 64], packed=[17, 1, 0, 4], max_slots=310, chunk=320, seed=r)
+    want = c.check()
+    for chunk in (1024, 1 << 30, (1 << 31) - 32):
+        c.ctx.set_decode_chunk(chunk)
+        for x, y in zip(c.run(), want):
+            assert np.array_equal(x, y), chunk

@@ -84,3 +84,34 @@ def test_page_tables_refuse_a_workspace_that_is_not_aligned():
     pool = B.PagePool(ints(16, 10), ints(16), ints(16), ints(40), ints(4))
     for workspace in (1028, 1032, 1025):
         assert ctx.pages_fit_status(pool, None, 1024, None, 1, 0, 16, None, workspace) == B.MTLA_ERR_INVALID_ARG
+
+
+CHUNKS = r"""
+#include "bounds.h"
+#include <climits>
+#include <initializer_list>
+int main() {
+  for (int live : {0, 1, 31, 32, 33, 640, INT_MAX - 1, INT_MAX})
+    for (int chunk : {32, 64, 96, 1024, 1 << 30, INT_MAX - 31})
+      if (mtla::chunks_of(live, chunk) != (live + (long long)chunk - 1) / chunk) return 1;
+  return 0;
+}
+"""
+
+
+@pytest.mark.skipif(not shutil.which("g++"), reason="no host compiler")
+def test_chunks_of_any_size(tmp_path):
+    (tmp_path / "main.cpp").write_text(CHUNKS)
+    subprocess.run(["g++", "-std=c++17", "-Wall", "-Werror", "-ftrapv", "-I", CSRC, str(tmp_path / "main.cpp"), "-o", str(tmp_path / "main")], check=True)
+    subprocess.run([str(tmp_path / "main")], check=True)
+
+
+@pytest.mark.parametrize("page_slots,n_pages", [(0, 0), (64, 40)])
+@pytest.mark.parametrize("max_slots", [1, 64, 65, 640])
+def test_workspace_for_a_chunk_that_holds_every_slot(max_slots, page_slots, n_pages):
+    ctx = B.Context(n_heads=8, d_head=64, r=256, d_rope=32, d_hyper=64, stride=2, max_batch=16, max_slots=max_slots, dtype="bf16", page_slots=page_slots, n_pages=n_pages)
+    sizes = []
+    for chunk in (1024, 1 << 30, (1 << 31) - 32):
+        ctx.set_decode_chunk(chunk)
+        sizes.append(ctx.workspace_bytes())
+    assert sizes[0] == sizes[1] == sizes[2]
