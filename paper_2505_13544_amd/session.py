@@ -563,17 +563,25 @@ class PackedSession:
         self._refusals(before)
         return scratch  # keep alive until the stream has consumed it
 
+    @staticmethod
+    def _bf16(out):
+        """Whether there is an output; the other sessions' is fp32, and would be filled by half with pairs of numbers."""
+        if getattr(out, "dtype", torch.bfloat16) != torch.bfloat16:
+            raise TypeError(f"out is bf16 here, not {out.dtype}")
+        return out is not None
+
     def decode(self, q, q_rope, *, out=None, out_latent=None, lse=None):
         """One query per sequence; out is bf16."""
-        self.ctx.decode_attn_packed(q, q_rope, self.w_uk, self.w_uv if out is not None else None, self.pool_c, self.pool_kr, self.seq_len,
-                                    self.table, self.cache, q.shape[0], out, out_latent, lse, self.workspace, self.stream)
+        w_uv = self.w_uv if self._bf16(out) else None
+        self.ctx.decode_attn_packed(q, q_rope, self.w_uk, w_uv, self.pool_c, self.pool_kr, self.seq_len, self.table, self.cache, q.shape[0], out,
+                                    out_latent, lse, self.workspace, self.stream)
 
     def step(self, c_new, kr_new, q, q_rope, *, out=None, out_latent=None, lse=None):
         """One step of incremental inference: tables, packing, the append of every sequence's token, attention; out is bf16."""
-        batch = len(q)
+        batch, w_uv = len(q), self.w_uv if self._bf16(out) else None  # (a refusal leaves the tables alone)
         self.fit(batch, 1)
         self.ctx.decode_step_packed(self.pool_c, self.pool_kr, self.tail_c, self.seq_len, self.table, self.cache, c_new, kr_new, self.hyp_A,
-                                    self.hyp_a, self.hyp_G, q, q_rope, self.w_uk, self.w_uv if out is not None else None, batch, out,
+                                    self.hyp_a, self.hyp_G, q, q_rope, self.w_uk, w_uv, batch, out,
                                     out_latent, lse, self.workspace, self.stream)
 
     def device_status(self) -> int:

@@ -46,3 +46,15 @@ def test_arrays_that_are_none_of_the_call(call):
     for kw in (dict(counts=ints(2)), dict(slot_map=longs(3, 3)), dict(slot_map=longs(11))):
         with pytest.raises(ValueError):
             getattr(s, call)(3, 4, **kw)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.float16])
+def test_outputs_of_another_type(dtype):
+    # refused before the tables are touched
+    s = session(3)
+    s.w_uv = None
+    x, out = torch.zeros(3, 4, 64, dtype=torch.bfloat16), torch.zeros(3, 4, 64, dtype=dtype)
+    with pytest.raises(TypeError):
+        s.decode(x, x, out=out)
+    with pytest.raises(TypeError):
+        s.step(x, x, x, x, out=out)
